@@ -428,6 +428,119 @@ int qconv_create_packed(qconv_handle** out, const qconv_desc* desc, const uint8_
 int qquantize_bias(const float* b_host, int K, int e_x, const int32_t* e_w_host,
                    int32_t* bias_q_host);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Operators for quantized language models.  Tensors are float32, bfloat16 or float16 (QTYPE_*), rows of values next to
+ * each other; row strides (ld_*) are in elements.  All calls are asynchronous on cuda_stream, may be captured into a CUDA
+ * graph, keep no scratch between calls, and read their device arguments only once the kernels before them in the
+ * stream are complete.  They launch on the current device, which must be the tensors'. */
+enum { QTYPE_F32 = 0, QTYPE_BF16 = 1, QTYPE_F16 = 2 };
+
+/* Microscaled 4-bit tensors: the (4, 1) type of Section 2.1 in blocks of 32 values along a row, each block with a
+ * scale of its own, 2^(s - 127) for a scale byte s.
+ *   codes   [rows][ceil(K / 32) * 16] bytes, two codes to a byte, the even-numbered value in the low half; rows are
+ *           filled up to whole blocks with code 0.  Code = sign bit, two exponent bits, one significand bit (Eq. 2); its
+ *           magnitudes are 0, 0.5, 1, 1.5, 2, 3, 4, 6.  16-byte aligned.
+ *   scales  QMX_ROWS:  [rows][ceil(K / 32)] bytes
+ *           QMX_TILES: tiles of 128 rows x 4 blocks, 512 bytes each, [ceil(rows / 128)][ceil(K / 128)] of them; the byte of
+ *           row r, block b is byte (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of its tile (the order the products read;
+ *           16-byte aligned).  Bytes of rows and blocks that only fill up a tile are written as 127.
+ * qmx_quantize: a block's scale is chosen from its largest finite magnitude,
+ *   QMX_COVER  the smallest e with 6 * 2^e >= that magnitude: nothing saturates (the rule of qscale_exponent)
+ *   QMX_FLOOR  e = floor(log2 of it) - 2: values above 6 * 2^e saturate (the rule of the OCP microscaling formats)
+ * with e >= -127; e = 0 for a block without a finite value but zero.  A value becomes the nearest code of value / 2^e,
+ * ties to the even pattern, saturating at 6; NaN becomes code 0, +-Inf +-6, and a zero magnitude is always code 0.
+ * qmx_dequantize: magnitude * 2^(s - 127) rounded to the output type (a byte of 255 reads as NaN).
+ * Byte counts: qmx_code_bytes, qmx_scale_bytes (0 for bad arguments).
+ * Limits: rows * ceil(K / 128) <= 2^30, rows counted in whole tiles for QMX_TILES. */
+enum { QMX_COVER = 0, QMX_FLOOR = 1 };
+enum { QMX_ROWS = 0, QMX_TILES = 1 };
+size_t qmx_code_bytes(long long rows, int K);
+size_t qmx_scale_bytes(long long rows, int K, int layout);
+int qmx_quantize(const void* d_x, int type, long long rows, int K, long long ld, int rule, int layout, uint8_t* d_codes,
+                 uint8_t* d_scales, void* cuda_stream);
+int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long rows, int K, int layout, void* d_y, int type,
+                   long long ld, void* cuda_stream);
+
+/* Inner-product layer on microscaled 4-bit operands:
+ *   y[t][n] = relu?(sum over k of x[t][k] w[n][k] + bias[n]),  t < tokens, n < N
+ * the sum in 32 bits on the tensor cores (its order is fixed by the sizes: the same call gives the same bits), rounded once to
+ * the output type.  Scales of both operands are in QMX_TILES.
+ *   d_w_codes, d_w_scales   the weights, N rows of K; d_bias N float32 or NULL.  They stay the caller's, are not copied,
+ *                           and must outlive the handle.
+ * A handle belongs to the device that is current when it is made; running it elsewhere is BAD_ARG.  It holds no scratch:
+ * runs may overlap on several streams, but one host thread uses it at a time.  Device-side waits are bounded as
+ * qconv_run's are; qmx_linear_status synchronises the stream of the last run and returns (and clears) the device status,
+ * qmx_linear_set_wait_limit is the test hook that qconv_set_wait_limit is. */
+typedef struct {
+  int N, K;
+  int relu;
+  int type;                     /* QTYPE_* of y */
+} qmx_linear_desc;
+typedef struct qmx_linear qmx_linear;
+int qmx_linear_create(qmx_linear** out, const qmx_linear_desc* desc, const uint8_t* d_w_codes, const uint8_t* d_w_scales,
+                      const float* d_bias);
+int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_scales, int tokens, void* d_y, long long ld,
+                   void* cuda_stream);
+int qmx_linear_status(qmx_linear* h);
+int qmx_linear_set_wait_limit(qmx_linear* h, unsigned int polls);
+int qmx_linear_describe(const qmx_linear* h, char* buf, size_t buf_len);
+int qmx_linear_destroy(qmx_linear* h);
+
+/* Residual addition, root-mean-square norm over the C values of a row, and conversion:
+ *   h = x + residual, rounded to the tensors' type (h = x without a residual); stored in d_sum if that is given
+ *   r = 1 / sqrt(mean(h^2) + eps), in float64, rounded to float32
+ *   y = (h * r) * gain, in float32
+ *   QNORM_I8       int8 codes [rows][C] of y at the given exponent e (qquantize_f32's conversion at 8 bits): the input of
+ *                  an int8 layer whose scale was calibrated
+ *   QNORM_I8_ROWS  the same at each row's own exponent, the smallest e >= -126 with 127 * 2^e >= the row's largest finite
+ *                  |y| (0 if that is 0); d_scales [rows] receives the byte e + 127
+ *   QNORM_MX       microscaled 4 bits (QMX_COVER), codes and scales as qmx_quantize writes them
+ * d_sum may be d_x or d_residual itself (with the same row stride); otherwise outputs overlap nothing.  Rows below
+ * 2^31, C up to 2^24, eps >= 0. */
+enum { QNORM_I8 = 0, QNORM_I8_ROWS = 1, QNORM_MX = 2 };
+typedef struct {
+  const void* d_x;
+  const void* d_residual;       /* or NULL */
+  const void* d_gain;           /* C values */
+  void* d_sum;                  /* or NULL */
+  int type;                     /* QTYPE_* of x, residual, gain and sum */
+  int C;
+  long long rows, ld_x, ld_residual, ld_sum;
+  double eps;
+  int out, e;                   /* QNORM_*; e: QNORM_I8 alone */
+  int layout;                   /* of the scales: QNORM_MX alone */
+  uint8_t* d_codes;
+  uint8_t* d_scales;            /* not QNORM_I8 */
+} qrmsnorm_args;
+int qrmsnorm(const qrmsnorm_args* args, void* cuda_stream);
+
+/* Quantized caches of keys and values: [num_slots] slots of `heads` heads of D values.  Pages are runs of slots: slot =
+ * page * page size + place in the page.
+ *   QCACHE_I8  codes [num_slots][heads][D] int8, scales [num_slots][heads]: the byte e + 127 of the head's exponent, the
+ *              smallest e >= -126 with 127 * 2^e >= its largest finite magnitude (0 if that is 0); values as qquantize_f32
+ *              converts them
+ *   QCACHE_MX  codes [num_slots][heads][ceil(D / 32) * 16], scales [num_slots][heads][ceil(D / 32)]: microscaled 4 bits
+ *              (QMX_COVER)
+ * qcache_write converts row i of keys (and values) into slot d_slots[i]; qcache_read brings slot d_slots[i] back to row
+ * i.  A slot outside [0, num_slots) skips its row: nothing is read or written for it (padded batches).  No slot may occur
+ * twice in one write (its contents would be undefined; no other slot is touched); reads may repeat slots.
+ * `values` may be NULL: a cache of one tensor.  The tensors' heads are D values next to each other, head_stride and
+ * token_stride elements apart (not negative); the rows that qcache_read writes must not overlap.  D <= 1024. */
+enum { QCACHE_I8 = 0, QCACHE_MX = 1 };
+typedef struct {
+  int format, heads, D;
+  long long num_slots;
+  uint8_t *d_k_codes, *d_k_scales, *d_v_codes, *d_v_scales;   /* the values' NULL for a cache of one tensor */
+} qcache_desc;
+typedef struct {
+  void* d_values;               /* read by qcache_write, written by qcache_read */
+  long long token_stride, head_stride;
+} qcache_values;
+int qcache_write(const qcache_desc* cache, const qcache_values* keys, const qcache_values* values, int type,
+                 const int64_t* d_slots, long long rows, void* cuda_stream);
+int qcache_read(const qcache_desc* cache, const int64_t* d_slots, long long rows, const qcache_values* keys,
+                const qcache_values* values, int type, void* cuda_stream);
+
 /* Checked build of the library (compiled with -DQCONV_CHECKED, binding.build_library(checked=True)): in the
  * CUDA-core kernels (conversions, pooling, packing, depthwise / direct convolution, eltwise, digit planes) every
  * global access with a computed address first tests its index against the tensor's extent; a failing test is

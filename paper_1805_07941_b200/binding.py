@@ -9,6 +9,7 @@ fallback.
 import ctypes
 import os
 import subprocess
+import tempfile
 
 import numpy as np
 
@@ -23,6 +24,11 @@ ERR_BAD_ARG, ERR_UNSUPPORTED_SHAPE, ERR_OVERFLOW_RISK, ERR_BAD_SHIFT = -1, -2, -
 ERR_RESIDUAL_SCALE, ERR_ALIGNMENT, ERR_CUDA, ERR_TIMEOUT = -5, -6, -7, -8
 ALGO_AUTO, ALGO_DIRECT, ALGO_IGEMM, ALGO_DEPTHWISE = 0, 1, 2, 3
 OUT_INT8, OUT_INT32, OUT_FLOAT = 0, 1, 2
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+MX_COVER, MX_FLOOR = 0, 1                    # rule of a block's scale
+MX_ROWS, MX_TILES = 0, 1                     # layout of the scales
+NORM_I8, NORM_I8_ROWS, NORM_MX = 0, 1, 2
+CACHE_I8, CACHE_MX = 0, 1
 
 
 class QconvError(RuntimeError):
@@ -58,6 +64,27 @@ class qcalib_stats(ctypes.Structure):
                 ("hist", ctypes.POINTER(ctypes.c_uint64))]
 
 
+class qmx_linear_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "K", "relu", "type")]
+
+
+class qrmsnorm_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("d_x", "d_residual", "d_gain", "d_sum")] + \
+        [(n, ctypes.c_int) for n in ("type", "C")] + \
+        [(n, ctypes.c_longlong) for n in ("rows", "ld_x", "ld_residual", "ld_sum")] + \
+        [("eps", ctypes.c_double)] + [(n, ctypes.c_int) for n in ("out", "e", "layout")] + \
+        [("d_codes", ctypes.c_void_p), ("d_scales", ctypes.c_void_p)]
+
+
+class qcache_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("format", "heads", "D")] + [("num_slots", ctypes.c_longlong)] + \
+        [(n, ctypes.c_void_p) for n in ("d_k_codes", "d_k_scales", "d_v_codes", "d_v_scales")]
+
+
+class qcache_values(ctypes.Structure):
+    _fields_ = [("d_values", ctypes.c_void_p), ("token_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong)]
+
+
 class qnet_step(ctypes.Structure):
     _fields_ = [("op", ctypes.c_int), ("n", ctypes.c_int), ("e_x", ctypes.c_int), ("n_bits", ctypes.c_int),
                 ("handle", ctypes.c_void_p), ("d_x", ctypes.c_void_p), ("d_residual", ctypes.c_void_p),
@@ -80,22 +107,29 @@ def sources():
 
 
 def build_library(force=False, verbose=False, checked=False):
-    """Compile csrc/qconv_api.cu for sm_100a into libqconv_b200.so beside this file (checked=True: the
-    -DQCONV_CHECKED variant, libqconv_b200_checked.so; load it by setting LIB_PATH before the first lib())."""
+    """Compile csrc/*.cu for sm_100a into libqconv_b200.so beside this file (checked=True: the -DQCONV_CHECKED variant,
+    libqconv_b200_checked.so; load it by setting LIB_PATH before the first lib()).  The translation units are compiled
+    side by side and linked."""
     srcs = sources()
     path = CHECKED_LIB_PATH if checked else LIB_PATH
     stale = (not os.path.exists(path)) or any(os.path.getmtime(s) > os.path.getmtime(path) for s in srcs)
     if not (force or stale):
         return path
     tmp = path + ".tmp%d" % os.getpid()
-    cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", tmp, os.path.join(_CSRC, "qconv_api.cu")]
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC"]
     if checked:
-        cmd.insert(1, "-DQCONV_CHECKED")
+        flags.insert(0, "-DQCONV_CHECKED")
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    subprocess.check_call(cmd)
+        flags += ["-Xptxas", "-v"]
+    with tempfile.TemporaryDirectory() as objects:
+        jobs = []
+        for src in (s for s in srcs if s.endswith(".cu")):
+            obj = os.path.join(objects, os.path.basename(src) + ".o")
+            jobs.append((obj, subprocess.Popen(["nvcc"] + flags + ["-c", "-o", obj, src])))
+        codes = [job.wait() for _, job in jobs]
+        if any(codes):
+            raise subprocess.CalledProcessError(next(c for c in codes if c), "nvcc")
+        subprocess.check_call(["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", tmp] + [obj for obj, _ in jobs])
     os.replace(tmp, path)
     return path
 
@@ -174,6 +208,26 @@ def lib():
         L.qgraph_set_input.argtypes = [vp, vp, vp]
         L.qgraph_inputs_destroy.argtypes = [vp]
         for name in ("qnet_run", "qgraph_record_begin", "qgraph_record_end", "qgraph_set_input", "qgraph_inputs_destroy"):
+            getattr(L, name).restype = ci
+        ll = ctypes.c_longlong
+        L.qmx_code_bytes.argtypes, L.qmx_code_bytes.restype = [ll, ci], sz
+        L.qmx_scale_bytes.argtypes, L.qmx_scale_bytes.restype = [ll, ci, ci], sz
+        L.qmx_quantize.argtypes = [vp, ci, ll, ci, ll, ci, ci, vp, vp, vp]
+        L.qmx_dequantize.argtypes = [vp, vp, ll, ci, ci, vp, ci, ll, vp]
+        L.qmx_linear_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(qmx_linear_desc), vp, vp, vp]
+        L.qmx_linear_run.argtypes = [vp, vp, vp, ci, vp, ll, vp]
+        L.qmx_linear_status.argtypes = [vp]
+        L.qmx_linear_set_wait_limit.argtypes = [vp, ctypes.c_uint]
+        L.qmx_linear_describe.argtypes = [vp, ctypes.c_char_p, sz]
+        L.qmx_linear_destroy.argtypes = [vp]
+        L.qrmsnorm.argtypes = [ctypes.POINTER(qrmsnorm_args), vp]
+        L.qcache_write.argtypes = [ctypes.POINTER(qcache_desc), ctypes.POINTER(qcache_values), ctypes.POINTER(qcache_values),
+                                   ci, vp, ll, vp]
+        L.qcache_read.argtypes = [ctypes.POINTER(qcache_desc), vp, ll, ctypes.POINTER(qcache_values),
+                                  ctypes.POINTER(qcache_values), ci, vp]
+        for name in ("qmx_quantize", "qmx_dequantize", "qmx_linear_create", "qmx_linear_run", "qmx_linear_status",
+                     "qmx_linear_set_wait_limit", "qmx_linear_describe", "qmx_linear_destroy", "qrmsnorm", "qcache_write",
+                     "qcache_read"):
             getattr(L, name).restype = ci
         L.qconv_checked_faults.argtypes = [ctypes.POINTER(ci)]
         L.qconv_checked_faults.restype = ci
@@ -593,3 +647,241 @@ def qquantize_bias(b, e_x, e_w):
     bq = np.zeros(b.shape, dtype=np.int32)
     _check(lib().qquantize_bias(bp, b.size, int(e_x), ep, _at(bq)))
     return bq
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Operators for quantized language models.  These check the tensors they are given (device, type, shape, strides): a
+# tensor on another device than the current one, or one that is too small, is a ValueError before anything runs.
+# ---------------------------------------------------------------------------------------------------------------
+_types = None
+
+
+def _type_of(dtype):
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+    t = _types.get(dtype)
+    if t is None:
+        raise ValueError("float32, bfloat16 or float16 tensors are wanted, not %s" % dtype)
+    return t
+
+
+def _on_device(*tensors):
+    """Every tensor (None: not given) on the current CUDA device."""
+    if _current_device is None:
+        _stream()
+    dev = _current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != dev):
+            raise ValueError("the tensors must be on the current CUDA device (%d), not on %s" % (dev, t.device))
+
+
+def _rows(t, what):
+    """Row stride of a 2-D tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("%s must be 2-D with contiguous rows" % what)
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _bytes(t, count, what):
+    """A contiguous tensor of at least `count` one-byte values."""
+    if t.element_size() != 1 or not t.is_contiguous() or t.numel() < count:
+        raise ValueError("%s must be a contiguous tensor of at least %d bytes" % (what, count))
+
+
+def _mx_size(rows, K, layout):
+    """(bytes of codes in a row, bytes of all scales) of a microscaled tensor."""
+    blocks = -(-K // 32)
+    return blocks * 16, -(-rows // 128) * -(-blocks // 4) * 512 if layout == MX_TILES else rows * blocks
+
+
+def qmx_quantize(x, rule=MX_COVER, layout=MX_TILES, codes=None, scales=None):
+    """Float CUDA tensor [rows, K] (contiguous rows, any row stride) -> (codes [rows, ceil(K / 32) * 16] uint8, scales):
+    microscaled 4-bit values in blocks of 32 along the row.  scales: uint8 [rows, ceil(K / 32)] for MX_ROWS, else the
+    tiles that QMXLinear reads (flat)."""
+    import torch
+    ld, (rows, K) = _rows(x, "x"), x.shape
+    pitch, size = _mx_size(rows, K, layout)
+    if codes is None:
+        codes = torch.empty((rows, pitch), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty((rows, pitch // 16) if layout == MX_ROWS else (size,), dtype=torch.uint8, device=x.device)
+    _on_device(x, codes, scales)
+    _bytes(codes, rows * pitch, "codes")
+    _bytes(scales, size, "scales")
+    if x.numel():
+        _check(lib().qmx_quantize(x.data_ptr(), _type_of(x.dtype), rows, K, ld, int(rule), int(layout), codes.data_ptr(),
+                                  scales.data_ptr(), _stream()))
+    return codes, scales
+
+
+def qmx_dequantize(codes, scales, K, layout=MX_TILES, dtype=None, out=None):
+    """Microscaled codes [rows, ...] and scales -> values [rows, K] of `dtype` (float32), or into `out`."""
+    import torch
+    rows = codes.shape[0]
+    if out is None:
+        out = torch.empty((rows, K), dtype=dtype or torch.float32, device=codes.device)
+    elif tuple(out.shape) != (rows, K):
+        raise ValueError("out must be [%d, %d]" % (rows, K))
+    pitch, size = _mx_size(rows, K, layout)
+    _on_device(codes, scales, out)
+    _bytes(codes, rows * pitch, "codes")
+    _bytes(scales, size, "scales")
+    if out.numel():
+        _check(lib().qmx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, int(K), int(layout), out.data_ptr(),
+                                    _type_of(out.dtype), _rows(out, "out"), _stream()))
+    return out
+
+
+class QMXLinear:
+    """An inner-product layer on microscaled 4-bit operands (qmx_linear_create / run / status / destroy): weights as
+    qmx_quantize(w [N, K], layout=MX_TILES) gives them, kept by this object and read where they lie."""
+
+    def __init__(self, w_codes, w_scales, N, K, bias=None, relu=0, dtype=None):
+        import torch
+        pitch, size = _mx_size(N, K, MX_TILES)
+        _on_device(w_codes, w_scales, bias)
+        _bytes(w_codes, N * pitch, "w_codes")
+        _bytes(w_scales, size, "w_scales")
+        if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != N):
+            raise ValueError("the bias must be %d contiguous float32 values" % N)
+        self.dtype = dtype or torch.bfloat16
+        self.desc = qmx_linear_desc(N=N, K=K, relu=int(relu), type=_type_of(self.dtype))
+        self.N, self.K, self._pitch = N, K, pitch
+        self._keep = (w_codes, w_scales, bias)
+        self.handle = ctypes.c_void_p()
+        _check(lib().qmx_linear_create(ctypes.byref(self.handle), ctypes.byref(self.desc), w_codes.data_ptr(), w_scales.data_ptr(),
+                                       _dev(bias)))
+        self._run = lib().qmx_linear_run
+
+    def run(self, x_codes, x_scales, y=None):
+        """x_codes [tokens, ...], x_scales in tiles -> y [tokens, N] (contiguous rows).  Asynchronous on the current stream."""
+        tokens = x_codes.shape[0]
+        if y is None:
+            import torch
+            y = torch.empty((tokens, self.N), dtype=self.dtype, device=x_codes.device)
+        _on_device(x_codes, x_scales, y)
+        _bytes(x_codes, tokens * self._pitch, "x_codes")
+        _bytes(x_scales, -(-tokens // 128) * -(-self._pitch // 64) * 512, "x_scales")
+        if y.dtype != self.dtype or y.shape != (tokens, self.N):
+            raise ValueError("y must be [%d, %d] of %s" % (tokens, self.N, self.dtype))
+        if tokens:
+            rc = self._run(self.handle, x_codes.data_ptr(), x_scales.data_ptr(), tokens, y.data_ptr(), _rows(y, "y"), _stream())
+            if rc:
+                _check(rc)
+        return y
+
+    def status(self):
+        return lib().qmx_linear_status(self.handle)
+
+    def set_wait_limit(self, polls):
+        _check(lib().qmx_linear_set_wait_limit(self.handle, int(polls)))
+
+    def describe(self):
+        buf = ctypes.create_string_buffer(200)
+        _check(lib().qmx_linear_describe(self.handle, buf, 200))
+        return buf.value.decode()
+
+    def destroy(self):
+        if self.handle:
+            lib().qmx_linear_destroy(self.handle)
+            self.handle = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def qrmsnorm(x, gain, eps, residual=None, sum_out=None, out=NORM_I8, e=0, layout=MX_TILES, codes=None, scales=None):
+    """Residual addition, root-mean-square norm and conversion of x [rows, C]: (codes, scales) with int8 codes at
+    exponent e (NORM_I8; scales None), int8 codes and a scale byte per row (NORM_I8_ROWS), or microscaled 4 bits
+    (NORM_MX).  sum_out receives x + residual and may be x or residual itself."""
+    import torch
+    ld, (rows, C) = _rows(x, "x"), x.shape
+    for t, what in ((residual, "residual"), (sum_out, "sum_out")):
+        if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
+            raise ValueError("%s must be like x" % what)
+    if gain.dtype != x.dtype or gain.shape != (C,) or not gain.is_contiguous():
+        raise ValueError("the gain must be %d contiguous values of x's type" % C)
+    pitch, size = _mx_size(rows, C, layout) if out == NORM_MX else (C, rows)
+    if codes is None:
+        codes = torch.empty((rows, pitch), dtype=torch.uint8 if out == NORM_MX else torch.int8, device=x.device)
+    if out == NORM_I8:
+        scales = None
+    elif scales is None:
+        shape = (rows, pitch // 16) if out == NORM_MX and layout == MX_ROWS else (size,)
+        scales = torch.empty(shape, dtype=torch.uint8, device=x.device)
+    _on_device(x, gain, residual, sum_out, codes, scales)
+    _bytes(codes, rows * pitch, "codes")
+    if scales is not None:
+        _bytes(scales, size, "scales")
+    if x.numel():
+        a = qrmsnorm_args(x.data_ptr(), _dev(residual), gain.data_ptr(), _dev(sum_out), _type_of(x.dtype), C, rows, ld,
+                          _rows(residual, "residual") if residual is not None else 0,
+                          _rows(sum_out, "sum_out") if sum_out is not None else 0, float(eps), int(out), int(e), int(layout),
+                          codes.data_ptr(), _dev(scales))
+        _check(lib().qrmsnorm(ctypes.byref(a), _stream()))
+    return codes, scales
+
+
+class QCache:
+    """A quantized cache of keys and values over tensors that the caller owns: codes [slots, heads, ...] and scales
+    [slots, heads, ...] of one byte each (the layout is qcache_desc's).  v_codes, v_scales None: a cache of one tensor."""
+
+    def __init__(self, k_codes, k_scales, v_codes=None, v_scales=None, D=None, fmt=CACHE_I8):
+        slots, heads = k_codes.shape[:2]
+        D = k_codes.shape[2] if D is None else D
+        blocks = -(-D // 32)
+        _on_device(k_codes, k_scales, v_codes, v_scales)
+        if (v_codes is None) != (v_scales is None):
+            raise ValueError("v_codes and v_scales belong together")
+        for c, s in ((k_codes, k_scales), (v_codes, v_scales)):
+            if c is not None:
+                _bytes(c, slots * heads * (D if fmt == CACHE_I8 else blocks * 16), "codes")
+                _bytes(s, slots * heads * (1 if fmt == CACHE_I8 else blocks), "scales")
+        self.slots, self.heads, self.D, self.fmt = slots, heads, D, fmt
+        self._keep = (k_codes, k_scales, v_codes, v_scales)
+        self.desc = qcache_desc(int(fmt), heads, D, slots, _dev(k_codes), _dev(k_scales), _dev(v_codes), _dev(v_scales))
+        self._desc = ctypes.byref(self.desc)
+
+    @classmethod
+    def empty(cls, slots, heads, D, fmt=CACHE_I8, values=True, device="cuda"):
+        """A cache over tensors of its own, all zeros."""
+        import torch
+        blocks = -(-D // 32)
+        width, per = (D, 1) if fmt == CACHE_I8 else (blocks * 16, blocks)
+        make = lambda n: torch.zeros((slots, heads, n), dtype=torch.uint8, device=device)
+        return cls(make(width), make(per), make(width) if values else None, make(per) if values else None, D=D, fmt=fmt)
+
+    k_codes, k_scales, v_codes, v_scales = (property(lambda self, i=i: self._keep[i]) for i in range(4))
+
+    def _values(self, t, rows, dtype):
+        if t.dim() != 3 or t.shape != (rows, self.heads, self.D) or t.dtype != dtype or (t.stride(2) != 1 and self.D > 1):
+            raise ValueError("keys and values must be [%d, %d, %d] of one type with contiguous heads" % (rows, self.heads, self.D))
+        return qcache_values(t.data_ptr(), t.stride(0), t.stride(1))
+
+    def _args(self, slots, k, v):
+        if slots.dim() != 1 or not slots.is_contiguous() or slots.element_size() != 8 or slots.is_floating_point():
+            raise ValueError("slots must be a contiguous 1-D int64 tensor")
+        if (v is None) != (self._keep[2] is None):
+            raise ValueError("the cache holds %s" % ("keys alone" if v is not None else "keys and values"))
+        _on_device(slots, k, v)
+        rows = slots.shape[0]
+        keys = self._values(k, rows, k.dtype)
+        return rows, _type_of(k.dtype), ctypes.byref(keys), ctypes.byref(self._values(v, rows, k.dtype)) if v is not None else None
+
+    def write(self, slots, k, v=None):
+        """Rows of k (and v) [rows, heads, D] into the slots; rows whose slot is outside the cache are skipped."""
+        rows, dtype, keys, values = self._args(slots, k, v)
+        if rows:
+            _check(lib().qcache_write(self._desc, keys, values, dtype, slots.data_ptr(), rows, _stream()))
+
+    def read(self, slots, k, v=None):
+        """The slots' keys (and values) into k (and v) [rows, heads, D]; rows whose slot is outside the cache stay as they are."""
+        rows, dtype, keys, values = self._args(slots, k, v)
+        if rows:
+            _check(lib().qcache_read(self._desc, slots.data_ptr(), rows, keys, values, dtype, _stream()))
+        return k, v

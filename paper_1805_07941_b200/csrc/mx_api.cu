@@ -1,0 +1,492 @@
+// Entry points of the operators on microscaled 4-bit tensors, norms and caches (include/qconv.h): argument checks, plans
+// and launches.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <new>
+
+#include "../../include/qconv.h"
+#include "kernel_mx_gemm.cuh"
+#include "kernels_cache.cuh"
+#include "kernels_mx.cuh"
+#include "kernels_norm.cuh"
+#include "library.cuh"
+#include "per_device.cuh"
+
+// The header's numbers and the kernels'.
+constexpr int kOfHeader[] = {QTYPE_F32, QTYPE_BF16, QTYPE_F16, QNORM_I8, QNORM_I8_ROWS, QNORM_MX, QCACHE_I8, QCACHE_MX};
+constexpr int kOfKernels[] = {qc::TYPE_F32, qc::TYPE_BF16, qc::TYPE_F16, qc::NORM_I8, qc::NORM_I8_ROWS, qc::NORM_MX, qc::CACHE_I8, qc::CACHE_MX};
+constexpr bool same_numbers() {
+  for (int i = 0; i < 8; ++i)
+    if (kOfHeader[i] != kOfKernels[i]) return false;
+  return true;
+}
+static_assert(same_numbers());
+
+using qc::fail;
+using qc::launch_chained;
+using qc::make_fastdiv;
+
+namespace {
+
+constexpr long long kMaxRows = 1ll << 40;
+constexpr long long kMaxUnits = 1ll << 30;        // pieces of a tensor that one launch counts in 31 bits
+
+size_t type_size(int type) { return type == QTYPE_F32 ? 4 : 2; }
+bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// Calls f with a value of the type that `type` stands for.
+template <typename F>
+auto with_type(int type, F&& f) {
+  if (type == QTYPE_BF16) return f(__nv_bfloat16());
+  if (type == QTYPE_F16) return f(__half());
+  return f(float());
+}
+bool type_ok(int type) { return type == QTYPE_F32 || type == QTYPE_BF16 || type == QTYPE_F16; }
+
+int check_mx(long long rows, int K, int layout) {
+  if (rows <= 0 || K <= 0) return fail(QCONV_ERR_BAD_ARG, "rows and K must be positive");
+  if (layout != QMX_ROWS && layout != QMX_TILES) return fail(QCONV_ERR_BAD_ARG, "unknown layout of scales %d", layout);
+  if (rows > kMaxRows || K > (1 << 28)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "tensor too large");
+  const long long padded = layout == QMX_TILES ? (rows + 127) / 128 * 128 : rows;
+  if (padded * ((K + 127ll) / 128) > kMaxUnits) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "tensor too large: more than 2^30 pieces of 128 values");
+  return QCONV_OK;
+}
+
+size_t scale_bytes(long long rows, int K, int layout) {
+  return layout == QMX_TILES ? static_cast<size_t>((rows + 127) / 128) * qc::mx_tiles_k(K) * qc::kMxTileBytes
+                             : static_cast<size_t>(rows) * qc::mx_blocks(K);
+}
+
+qc::MxScales make_scales(uint8_t* bytes, long long rows, int K, int layout) {
+  return {bytes, layout == QMX_TILES, qc::mx_blocks(K), qc::mx_tiles_k(K), scale_bytes(rows, K, layout)};
+}
+
+int check_code_alignment(const void* codes, const void* scales, int layout) {
+  if (!aligned(codes, 16)) return fail(QCONV_ERR_ALIGNMENT, "codes must be 16-byte aligned");
+  if (layout == QMX_TILES && !aligned(scales, 16)) return fail(QCONV_ERR_ALIGNMENT, "scales in tiles must be 16-byte aligned");
+  return QCONV_OK;
+}
+
+int check_values(const void* p, int type, long long ld, int width, const char* what) {
+  if (ld < width) return fail(QCONV_ERR_BAD_ARG, "row stride of %s is below the row's length", what);
+  if (ld > kMaxRows) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "row stride of %s too large", what);
+  if (!aligned(p, type_size(type))) return fail(QCONV_ERR_ALIGNMENT, "%s must be aligned to its type", what);
+  return QCONV_OK;
+}
+// Rows of eight-value vectors at 16-byte boundaries.
+int vectors_ok(const void* p, int type, long long ld) { return aligned(p, 16) && ld * type_size(type) % 16 == 0; }
+
+}  // namespace
+
+namespace qc {
+cudaError_t mx_checked_faults(int (&v)[2]) {
+  v[0] = v[1] = 0;
+#ifdef QCONV_CHECKED
+  cudaError_t e = cudaMemcpyFromSymbol(v, g_checked_fault, sizeof(v));
+  const int zero[2] = {0, 0};
+  if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_checked_fault, zero, sizeof(zero));
+  return e;
+#else
+  return cudaSuccess;
+#endif
+}
+}  // namespace qc
+
+extern "C" {
+
+// --------------------------------------------------------------------------- microscaled tensors
+size_t qmx_code_bytes(long long rows, int K) {
+  return rows <= 0 || K <= 0 ? 0 : static_cast<size_t>(rows) * qc::mx_blocks(K) * 16;
+}
+
+size_t qmx_scale_bytes(long long rows, int K, int layout) {
+  if (rows <= 0 || K <= 0 || (layout != QMX_ROWS && layout != QMX_TILES)) return 0;
+  return scale_bytes(rows, K, layout);
+}
+
+int qmx_quantize(const void* d_x, int type, long long rows, int K, long long ld, int rule, int layout, uint8_t* d_codes,
+                 uint8_t* d_scales, void* cuda_stream) {
+  if (!d_x || !d_codes || !d_scales) return fail(QCONV_ERR_BAD_ARG, "NULL tensor pointer");
+  if (!type_ok(type)) return fail(QCONV_ERR_BAD_ARG, "unknown type %d", type);
+  if (rule != QMX_COVER && rule != QMX_FLOOR) return fail(QCONV_ERR_BAD_ARG, "unknown rule %d", rule);
+  int rc = check_mx(rows, K, layout);
+  if (!rc) rc = check_values(d_x, type, ld, K, "x");
+  if (!rc) rc = check_code_alignment(d_codes, d_scales, layout);
+  if (rc) return rc;
+  const int pieces = (K + 127) / 128;
+  const int units = static_cast<int>((layout == QMX_TILES ? (rows + 127) / 128 * 128 : rows) * pieces);
+  const int grid = qc::grid_for((units + 15ll) / 16, 1, 148 * 8);
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    CUDA_TRY(launch_chained(qc::mx_quantize_kernel<T>, dim3(grid), dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream),
+                            static_cast<const T*>(d_x), static_cast<size_t>(ld), static_cast<size_t>(rows), K, d_codes,
+                            make_scales(d_scales, rows, K, layout), rule == QMX_COVER ? 0x3FFFFFu : 0u, units, make_fastdiv(pieces),
+                            vectors_ok(d_x, type, ld)));
+    return static_cast<int>(QCONV_OK);
+  });
+}
+
+int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long rows, int K, int layout, void* d_y, int type, long long ld,
+                   void* cuda_stream) {
+  if (!d_y || !d_codes || !d_scales) return fail(QCONV_ERR_BAD_ARG, "NULL tensor pointer");
+  if (!type_ok(type)) return fail(QCONV_ERR_BAD_ARG, "unknown type %d", type);
+  int rc = check_mx(rows, K, layout);
+  if (!rc) rc = check_values(d_y, type, ld, K, "y");
+  if (!rc) rc = check_code_alignment(d_codes, d_scales, layout);
+  if (rc) return rc;
+  const int pieces = (K + 127) / 128;
+  const int units = static_cast<int>(rows * pieces);
+  const int grid = qc::grid_for((units + 15ll) / 16, 1, 148 * 8);
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    CUDA_TRY(launch_chained(qc::mx_dequantize_kernel<T>, dim3(grid), dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream),
+                            d_codes, make_scales(const_cast<uint8_t*>(d_scales), rows, K, layout), static_cast<size_t>(rows), K,
+                            static_cast<T*>(d_y), static_cast<size_t>(ld), units, make_fastdiv(pieces), vectors_ok(d_y, type, ld)));
+    return static_cast<int>(QCONV_OK);
+  });
+}
+
+// --------------------------------------------------------------------------- products
+}  // extern "C"
+
+struct qmx_linear {
+  qmx_linear_desc d;
+  const uint8_t* w_codes;
+  const uint8_t* w_scales;
+  const float* bias;
+  DevicePool::Block block;
+  int* d_status = nullptr;
+  int device = 0, num_sms = 148;
+  CUtensorMap map_w, map_ws, map_x, map_xs;
+  const uint8_t* x_codes = nullptr;      // what map_x and map_xs are of
+  const uint8_t* x_scales = nullptr;
+  int x_tokens = 0, x_bn = 0;
+  int bn = 0, split = 0, stages = 0;     // the last run's form
+  unsigned int wait_limit = 1u << 22;
+  cudaStream_t last_stream = nullptr;
+};
+
+namespace {
+
+int encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, cuuint64_t inner, cuuint64_t rows, cuuint64_t pitch,
+              cuuint32_t box_inner, cuuint32_t box_rows, CUtensorMapSwizzle swizzle) {
+  const qc::EncodeTiledFn fn = qc::get_encode_fn();
+  if (!fn) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+  const cuuint64_t dims[2] = {inner, rows}, strides[1] = {pitch};
+  const cuuint32_t box[2] = {box_inner, box_rows}, steps[2] = {1, 1};
+  const CUresult r = fn(map, type, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
+  return QCONV_OK;
+}
+// Codes [rows][K] in boxes of `box_rows` rows x 256 values, and their scale tiles in boxes of two tiles along the
+// contraction x box_rows / 128 (what a box reaches beyond the arrays is read as zeros).
+int encode_operand(CUtensorMap* codes, CUtensorMap* scales, const uint8_t* d_codes, const uint8_t* d_scales, int rows, int K, int box_rows) {
+  const cuuint64_t pitch = static_cast<cuuint64_t>(qc::mx_blocks(K)) * 16, tiles = qc::mx_tiles_k(K);
+  int rc = encode_2d(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, d_codes, pitch, rows, pitch, qc::kMxStageBytes, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+  if (!rc)
+    rc = encode_2d(scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, d_scales, tiles * 128, (rows + 127) / 128, tiles * qc::kMxTileBytes, 256,
+                   (box_rows + 127) / 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+  return rc;
+}
+
+template <int BN, typename Y>
+cudaError_t allow_gemm_smem() {
+  return cudaFuncSetAttribute(qc::mx_gemm_kernel<BN, Y>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+}
+
+template <int BN, typename Y>
+int launch_gemm(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
+  using Tile = qc::MxTile<BN>;
+  static qc::PerDevice<cudaError_t> allowed;
+  CUDA_TRY(allowed.once(h->device, allow_gemm_smem<BN, Y>));
+  const int per_cta = (prm.k_stages + prm.split - 1) / prm.split;
+  // two CTAs an SM where their columns of tensor memory and a ring worth having fit, so that one drains while the other multiplies
+  const uint32_t room = (Tile::kCols <= 256 ? 113u : 227u) * 1024 - 1024 - sizeof(qc::MxGemmShared);
+  prm.stages = std::max(2, std::min({per_cta, static_cast<int>(room / Tile::kStage), qc::kMxMaxStages}));
+  prm.ring_bytes = prm.stages * Tile::kStage;
+  if (prm.split > 1) prm.ring_bytes = std::max<uint32_t>(prm.ring_bytes, BN * 512);
+  const size_t smem = 1024 + prm.ring_bytes + sizeof(qc::MxGemmShared);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned int>(prm.tiles_n) * prm.tiles_t * prm.split);
+  cfg.blockDim = dim3(qc::kMxGemmThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = qc::chained_launches() ? 1 : 0;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = prm.split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = prm.split > 1 ? 2 : 1;
+  h->bn = BN; h->split = prm.split; h->stages = prm.stages;
+  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_kernel<BN, Y>, h->map_w, h->map_x, h->map_ws, h->map_xs, prm, h->bias, y, h->d_status,
+                              h->wait_limit));
+  return QCONV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qmx_linear_create(qmx_linear** out, const qmx_linear_desc* desc, const uint8_t* d_w_codes, const uint8_t* d_w_scales, const float* d_bias) {
+  if (!out) return fail(QCONV_ERR_BAD_ARG, "out is NULL");
+  *out = nullptr;
+  if (!desc || !d_w_codes || !d_w_scales) return fail(QCONV_ERR_BAD_ARG, "desc, d_w_codes or d_w_scales is NULL");
+  if (!type_ok(desc->type)) return fail(QCONV_ERR_BAD_ARG, "unknown type %d", desc->type);
+  int rc = check_mx(desc->N, desc->K, QMX_TILES);
+  if (!rc) rc = check_code_alignment(d_w_codes, d_w_scales, QMX_TILES);
+  if (rc) return rc;
+  if (!aligned(d_bias, 4)) return fail(QCONV_ERR_ALIGNMENT, "the bias must be aligned to its type");
+  qmx_linear* h = new (std::nothrow) qmx_linear();
+  if (!h) return fail(QCONV_ERR_CUDA, "qmx_linear_create: out of host memory");
+  h->d = *desc;
+  h->w_codes = d_w_codes; h->w_scales = d_w_scales; h->bias = d_bias;
+  rc = encode_operand(&h->map_w, &h->map_ws, d_w_codes, d_w_scales, desc->N, desc->K, 128);
+  cudaError_t e = cudaGetDevice(&h->device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
+  if (!rc && e == cudaSuccess) e = DevicePool::pool().take(&h->block, sizeof(int));
+  if (!rc && e == cudaSuccess) {
+    h->d_status = static_cast<int*>(h->block.ptr);
+    const int zero = 0;
+    e = cudaMemcpy(h->d_status, &zero, sizeof(int), cudaMemcpyHostToDevice);
+  }
+  if (!rc && e != cudaSuccess) rc = fail(QCONV_ERR_CUDA, "qmx_linear_create: %s", cudaGetErrorString(e));
+  if (rc) { delete h; return rc; }
+  *out = h;
+  return QCONV_OK;
+}
+
+int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_scales, int tokens, void* d_y, long long ld, void* cuda_stream) {
+  if (!h || !d_x_codes || !d_x_scales || !d_y) return fail(QCONV_ERR_BAD_ARG, "NULL handle or tensor pointer");
+  const qmx_linear_desc& d = h->d;
+  int rc = check_mx(tokens, d.K, QMX_TILES);
+  if (!rc) rc = check_code_alignment(d_x_codes, d_x_scales, QMX_TILES);
+  if (!rc) rc = check_values(d_y, d.type, ld, d.N, "y");
+  if (rc) return rc;
+  int dev = 0;
+  CUDA_TRY(cudaGetDevice(&dev));
+  if (dev != h->device) return fail(QCONV_ERR_BAD_ARG, "the handle belongs to device %d, the current device is %d", h->device, dev);
+  qc::MxGemmParams prm = {};
+  prm.N = d.N; prm.T = tokens; prm.ld = static_cast<size_t>(ld); prm.relu = d.relu != 0;
+  prm.k_tiles = qc::mx_tiles_k(d.K);
+  prm.k_stages = (prm.k_tiles + 1) / 2;
+  prm.tiles_n = (d.N + 127) / 128;
+  const int bn = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+  prm.tiles_t = (tokens + bn - 1) / bn;
+  if (static_cast<long long>(prm.tiles_n) * prm.tiles_t > (1ll << 27)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "product too large");
+  const int tiles = prm.tiles_n * prm.tiles_t;
+  prm.split = 1;
+  while (prm.split < 8 && tiles * prm.split * 2 <= h->num_sms && prm.split * 2 <= prm.k_stages) prm.split *= 2;
+  if (h->x_codes != d_x_codes || h->x_scales != d_x_scales || h->x_tokens != tokens || h->x_bn != bn) {
+    h->x_codes = nullptr;
+    rc = encode_operand(&h->map_x, &h->map_xs, d_x_codes, d_x_scales, tokens, d.K, bn);
+    if (rc) return rc;
+    h->x_codes = d_x_codes; h->x_scales = d_x_scales; h->x_tokens = tokens; h->x_bn = bn;
+  }
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  h->last_stream = st;
+  return with_type(d.type, [&](auto t) {
+    using Y = decltype(t);
+    Y* y = static_cast<Y*>(d_y);
+    if (bn == 16) return launch_gemm<16, Y>(h, prm, y, st);
+    if (bn == 32) return launch_gemm<32, Y>(h, prm, y, st);
+    if (bn == 64) return launch_gemm<64, Y>(h, prm, y, st);
+    return launch_gemm<128, Y>(h, prm, y, st);
+  });
+}
+
+int qmx_linear_status(qmx_linear* h) {
+  if (!h) return fail(QCONV_ERR_BAD_ARG, "NULL handle");
+  CUDA_TRY(cudaStreamSynchronize(h->last_stream));
+  int st = 0;
+  CUDA_TRY(cudaMemcpy(&st, h->d_status, sizeof(int), cudaMemcpyDeviceToHost));
+  if (st != 0) {
+    CUDA_TRY(cudaMemset(h->d_status, 0, sizeof(int)));
+    return fail(st, "a bounded device-side wait expired (status %d)", st);
+  }
+  return QCONV_OK;
+}
+
+int qmx_linear_set_wait_limit(qmx_linear* h, unsigned int polls) {
+  if (!h) return fail(QCONV_ERR_BAD_ARG, "NULL handle");
+  h->wait_limit = polls;
+  return QCONV_OK;
+}
+
+int qmx_linear_describe(const qmx_linear* h, char* buf, size_t buf_len) {
+  if (!h || !buf || buf_len == 0) return fail(QCONV_ERR_BAD_ARG, "NULL argument");
+  snprintf(buf, buf_len, "mx N=%d K=%d tile=128x%d split=%d stages=%d", h->d.N, h->d.K, h->bn, h->split, h->stages);
+  return QCONV_OK;
+}
+
+int qmx_linear_destroy(qmx_linear* h) {
+  if (!h) return fail(QCONV_ERR_BAD_ARG, "NULL handle");
+  delete h;
+  return QCONV_OK;
+}
+
+// --------------------------------------------------------------------------- norm
+}  // extern "C"
+
+namespace {
+
+template <typename T, int OUT, int W, int V>
+int launch_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
+  constexpr int threads = qc::kNormThreads<W>, rows = threads / (32 * W);
+  CUDA_TRY(launch_chained(qc::rmsnorm_kernel<T, OUT, W, V>, dim3(static_cast<unsigned int>((a.rows + rows - 1) / rows)), dim3(threads), 0, st, a));
+  return QCONV_OK;
+}
+
+template <typename T, int OUT>
+int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
+  if (a.C <= 256) return launch_norm<T, OUT, 1, 1>(a, st);
+  if (a.C <= 1024) return a.rows >= 1024 ? launch_norm<T, OUT, 1, 4>(a, st) : launch_norm<T, OUT, 4, 1>(a, st);
+  if (a.rows < 512) {
+    if (a.C <= 4096) return launch_norm<T, OUT, 16, 1>(a, st);
+    if (a.C <= 8192) return launch_norm<T, OUT, 32, 1>(a, st);
+  }
+  if (a.C <= 4096) return launch_norm<T, OUT, 4, 4>(a, st);
+  if (a.C <= 8192) return launch_norm<T, OUT, 8, 4>(a, st);
+  if (a.C <= 16384) return launch_norm<T, OUT, 16, 4>(a, st);
+  CUDA_TRY(launch_chained(qc::rmsnorm_long_kernel<T, OUT>, dim3(static_cast<unsigned int>(a.rows)), dim3(32 * qc::kNormLongWarps), 0, st, a));
+  return QCONV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qrmsnorm(const qrmsnorm_args* args, void* cuda_stream) {
+  if (!args) return fail(QCONV_ERR_BAD_ARG, "args is NULL");
+  const qrmsnorm_args& g = *args;
+  if (!g.d_x || !g.d_gain || !g.d_codes) return fail(QCONV_ERR_BAD_ARG, "NULL tensor pointer");
+  if (!type_ok(g.type)) return fail(QCONV_ERR_BAD_ARG, "unknown type %d", g.type);
+  if (g.out != QNORM_I8 && g.out != QNORM_I8_ROWS && g.out != QNORM_MX) return fail(QCONV_ERR_BAD_ARG, "unknown output %d", g.out);
+  if (g.rows <= 0 || g.C <= 0) return fail(QCONV_ERR_BAD_ARG, "rows and C must be positive");
+  if (g.rows > 0x7FFFFFFFll || g.C > (1 << 24)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "tensor too large: rows below 2^31, C up to 2^24");
+  if (!(g.eps >= 0.0) || std::isinf(g.eps)) return fail(QCONV_ERR_BAD_ARG, "eps must be finite and not negative");
+  if (g.out == QNORM_I8 && (g.e < -126 || g.e > 126)) return fail(QCONV_ERR_BAD_ARG, "exponent %d outside [-126, 126]", g.e);
+  if (g.out != QNORM_I8 && !g.d_scales) return fail(QCONV_ERR_BAD_ARG, "this output needs d_scales");
+  int rc = check_values(g.d_x, g.type, g.ld_x, g.C, "x");
+  if (!rc && g.d_residual) rc = check_values(g.d_residual, g.type, g.ld_residual, g.C, "the residual");
+  if (!rc && g.d_sum) rc = check_values(g.d_sum, g.type, g.ld_sum, g.C, "the sum");
+  if (!rc && !aligned(g.d_gain, type_size(g.type))) rc = fail(QCONV_ERR_ALIGNMENT, "the gain must be aligned to its type");
+  if (!rc && g.out == QNORM_MX) {
+    rc = check_mx(g.rows, g.C, g.layout);
+    if (!rc) rc = check_code_alignment(g.d_codes, g.d_scales, g.layout);
+  }
+  if (rc) return rc;
+  if (g.d_sum && ((g.d_sum == g.d_x && g.ld_sum != g.ld_x) || (g.d_sum == g.d_residual && g.ld_sum != g.ld_residual)))
+    return fail(QCONV_ERR_BAD_ARG, "a sum in place of an input needs that input's row stride");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return with_type(g.type, [&](auto t) {
+    using T = decltype(t);
+    qc::NormArgs<T> a = {};
+    a.x = static_cast<const T*>(g.d_x); a.residual = static_cast<const T*>(g.d_residual); a.gain = static_cast<const T*>(g.d_gain);
+    a.sum = static_cast<T*>(g.d_sum);
+    a.ld_x = g.ld_x; a.ld_res = g.d_residual ? g.ld_residual : 0; a.ld_sum = g.d_sum ? g.ld_sum : 0;
+    a.rows = g.rows; a.C = g.C; a.eps = g.eps;
+    a.vec_ok = vectors_ok(g.d_x, g.type, g.ld_x) && aligned(g.d_gain, 16) && (!g.d_residual || vectors_ok(g.d_residual, g.type, g.ld_residual)) &&
+               (!g.d_sum || vectors_ok(g.d_sum, g.type, g.ld_sum));
+    a.code_vec = aligned(g.d_codes, 8) && g.C % 8 == 0;
+    a.inv = std::ldexp(1.0f, -g.e);
+    a.codes = g.d_codes;
+    if (g.out == QNORM_MX) a.scales = make_scales(g.d_scales, g.rows, g.C, g.layout);
+    else a.scales.bytes = g.d_scales;
+    if (g.out == QNORM_I8) return run_norm<T, qc::NORM_I8>(a, st);
+    if (g.out == QNORM_I8_ROWS) return run_norm<T, qc::NORM_I8_ROWS>(a, st);
+    return run_norm<T, qc::NORM_MX>(a, st);
+  });
+}
+
+// --------------------------------------------------------------------------- caches
+}  // extern "C"
+
+namespace {
+
+// Checks and the kernels' arguments, the same for both directions.
+int cache_args(const qcache_desc* c, const qcache_values* keys, const qcache_values* values, int type, const int64_t* d_slots, long long rows,
+               qc::CacheArgs* a) {
+  if (!c || !keys || !d_slots) return fail(QCONV_ERR_BAD_ARG, "cache, keys or d_slots is NULL");
+  if (c->format != QCACHE_I8 && c->format != QCACHE_MX) return fail(QCONV_ERR_BAD_ARG, "unknown format %d", c->format);
+  if (!type_ok(type)) return fail(QCONV_ERR_BAD_ARG, "unknown type %d", type);
+  if (c->num_slots <= 0 || c->heads <= 0 || c->D <= 0 || rows < 0) return fail(QCONV_ERR_BAD_ARG, "num_slots, heads and D must be positive, rows not negative");
+  if (c->D > 1024) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "D is at most 1024");
+  if (c->heads > (1 << 20) || c->num_slots > (1ll << 40)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "cache too large");
+  a->sides = values ? 2 : 1;
+  if (rows > kMaxUnits / c->heads / a->sides) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "more than 2^30 heads in one call");
+  if (!aligned(d_slots, 8)) return fail(QCONV_ERR_ALIGNMENT, "slots must be aligned to their type");
+  a->slots = reinterpret_cast<const long long*>(d_slots);
+  a->num_slots = c->num_slots; a->heads = c->heads; a->D = c->D; a->blocks = qc::mx_blocks(c->D);
+  a->items = static_cast<int>(rows * c->heads * a->sides);
+  a->fd_heads = make_fastdiv(c->heads);
+  a->code_pitch = c->format == QCACHE_I8 ? c->D : a->blocks * 16;
+  a->scale_pitch = c->format == QCACHE_I8 ? 1 : a->blocks;
+  a->vec_ok = 1;
+  a->code_vec = c->D % 8 == 0;
+  const qcache_values* in[2] = {keys, values};
+  uint8_t* codes[2] = {c->d_k_codes, c->d_v_codes};
+  uint8_t* scales[2] = {c->d_k_scales, c->d_v_scales};
+  for (int i = 0; i < a->sides; ++i) {
+    const qcache_values& v = *in[i];
+    if (!v.d_values || !codes[i] || !scales[i]) return fail(QCONV_ERR_BAD_ARG, "NULL tensor pointer");
+    if (v.token_stride < 0 || v.head_stride < 0 || v.token_stride > kMaxRows || v.head_stride > kMaxRows)
+      return fail(QCONV_ERR_BAD_ARG, "strides must not be negative, nor above 2^40");
+    if (!aligned(v.d_values, type_size(type))) return fail(QCONV_ERR_ALIGNMENT, "values must be aligned to their type");
+    if (c->format == QCACHE_MX && !aligned(codes[i], 16)) return fail(QCONV_ERR_ALIGNMENT, "codes must be 16-byte aligned");
+    a->side[i] = {codes[i], scales[i], v.d_values, v.token_stride, v.head_stride};
+    a->vec_ok &= vectors_ok(v.d_values, type, v.token_stride) && v.head_stride * type_size(type) % 16 == 0;
+    a->code_vec &= aligned(codes[i], 8);
+  }
+  return QCONV_OK;
+}
+
+template <typename T, int FMT, int LANES, int V>
+int launch_cache(const qc::CacheArgs& a, bool write, cudaStream_t st) {
+  constexpr int per_block = qc::kCacheThreads / LANES;
+  if (write)
+    CUDA_TRY(launch_chained(qc::cache_write_kernel<T, FMT, LANES, V>, dim3(qc::grid_for(a.items, per_block, 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));
+  else
+    CUDA_TRY(launch_chained(qc::cache_read_kernel<T, FMT, LANES, V>, dim3(qc::grid_for(a.items, per_block, 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));
+  return QCONV_OK;
+}
+template <typename T, int FMT>
+int run_cache(const qc::CacheArgs& a, bool write, cudaStream_t st) {
+  if (a.D <= 64) return launch_cache<T, FMT, 8, 1>(a, write, st);
+  if (a.D <= 128) return launch_cache<T, FMT, 16, 1>(a, write, st);
+  if (a.D <= 256) return launch_cache<T, FMT, 32, 1>(a, write, st);
+  return launch_cache<T, FMT, 32, 4>(a, write, st);
+}
+int run_cache(const qcache_desc* c, const qcache_values* keys, const qcache_values* values, int type, const int64_t* d_slots, long long rows,
+              bool write, void* cuda_stream) {
+  qc::CacheArgs a = {};
+  const int rc = cache_args(c, keys, values, type, d_slots, rows, &a);
+  if (rc || a.items == 0) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    return c->format == QCACHE_I8 ? run_cache<T, qc::CACHE_I8>(a, write, st) : run_cache<T, qc::CACHE_MX>(a, write, st);
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+int qcache_write(const qcache_desc* cache, const qcache_values* keys, const qcache_values* values, int type, const int64_t* d_slots,
+                 long long rows, void* cuda_stream) {
+  return run_cache(cache, keys, values, type, d_slots, rows, true, cuda_stream);
+}
+
+int qcache_read(const qcache_desc* cache, const int64_t* d_slots, long long rows, const qcache_values* keys, const qcache_values* values,
+                int type, void* cuda_stream) {
+  return run_cache(cache, keys, values, type, d_slots, rows, false, cuda_stream);
+}
+
+}  // extern "C"

@@ -30,47 +30,21 @@
 #include "kernels_npconv.cuh"
 #include "kernels_simple.cuh"
 #include "kernels_threshold.cuh"
+#include "library.cuh"
 #include "per_device.cuh"
 
 static_assert(QCALIB_STATIC_MAX_BINS <= qc::kCalibMaxBins, "built-in scratch holds kCalibMaxBins counters");
 
+using qc::fail;
+using qc::get_encode_fn;
+using qc::grid_for;
+using qc::launch_chained;
+using qc::make_fastdiv;
+using qc::EncodeTiledFn;
+
 namespace {
 
 thread_local char g_err[512] = "";
-
-int fail(int code, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof(g_err), fmt, ap);
-  va_end(ap);
-  return code;
-}
-
-#define CUDA_TRY(expr)                                                                        \
-  do {                                                                                        \
-    cudaError_t e_ = (expr);                                                                  \
-    if (e_ != cudaSuccess)                                                                    \
-      return fail(QCONV_ERR_CUDA, "%s failed: %s", #expr, cudaGetErrorString(e_));            \
-  } while (0)
-
-// cuTensorMapEncodeTiled is resolved through the runtime so the library links only cudart.
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-        qres == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  });
-  return fn;
-}
 
 CUtensorMapSwizzle swizzle_for(int bkc) {
   if (bkc == 0) return CU_TENSOR_MAP_SWIZZLE_NONE;
@@ -106,98 +80,32 @@ inline bool is_window_mode(int m) { return m == MODE_S2D || m == MODE_WROW; }
 
 }  // namespace
 
-// Device memory of the handles' tables and scratch.  A network's calibration builds and destroys two handles per layer;
-// cudaMalloc and cudaFree took two thirds of that time, and at times a hundred milliseconds for one call.  Blocks given back are kept for the next handle, at most kKeep bytes per
-// device, and all of them are freed when the last block in use is given back, or when the device has no memory left.  Any thread, any stream: a block is only
-// given back after the device is idle, so whoever takes it next may overwrite it at once.
-class DevicePool {
- public:
-  struct Block {
-    void* ptr = nullptr;
-    size_t bytes = 0;
-    int device = 0;
-    Block() = default;
-    Block(const Block&) = delete;
-    Block& operator=(const Block&) = delete;
-    ~Block() { if (ptr) pool().give(*this); }
-  };
-  static DevicePool& pool() {
-    static DevicePool* p = new DevicePool;                 // never destroyed: handles may outlive static destructors
-    return *p;
-  }
-  cudaError_t take(Block* b, size_t bytes) {
-    bytes = (std::max<size_t>(bytes, 1) + 4095) / 4096 * 4096;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    b->device = dev;
-    std::lock_guard<std::mutex> lock(mu_);
-    PerDevice& d = per_device_[dev & 63];
-    size_t best = d.free.size();
-    for (size_t i = 0; i < d.free.size(); ++i)
-      if (d.free[i].second >= bytes && d.free[i].second <= 2 * bytes && (best == d.free.size() || d.free[i].second < d.free[best].second))
-        best = i;
-    if (best < d.free.size()) {
-      b->ptr = d.free[best].first;
-      b->bytes = d.free[best].second;
-      d.kept -= b->bytes;
-      d.free.erase(d.free.begin() + static_cast<long>(best));
-    } else {
-      e = allocate(&b->ptr, bytes, d);
-      if (e != cudaSuccess) { b->ptr = nullptr; return e; }
-      b->bytes = bytes;
-    }
-    ++d.live;
-    return cudaSuccess;
-  }
-  // cudaMalloc for memory that is not the pool's.
-  template <typename T>
-  cudaError_t plain(T** ptr, size_t bytes) {
-    int dev = 0;
-    const cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    std::lock_guard<std::mutex> lock(mu_);
-    return allocate(reinterpret_cast<void**>(ptr), bytes, per_device_[dev & 63]);
-  }
+namespace qc {
 
- private:
-  static constexpr size_t kKeep = 256u << 20;
-  struct PerDevice {
-    std::vector<std::pair<void*, size_t>> free;            // oldest first
-    size_t kept = 0, live = 0;
-  };
-  std::mutex mu_;
-  PerDevice per_device_[64];
+int fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof(g_err), fmt, ap);
+  va_end(ap);
+  return code;
+}
 
-  // On a full device what is kept for later handles goes first.  (Kept blocks are idle.)
-  cudaError_t allocate(void** ptr, size_t bytes, PerDevice& d) {
-    cudaError_t e = cudaMalloc(ptr, bytes);
-    if (e != cudaErrorMemoryAllocation || d.free.empty()) return e;
-    cudaGetLastError();
-    for (auto& f : d.free) cudaFree(f.first);
-    d.free.clear();
-    d.kept = 0;
-    return cudaMalloc(ptr, bytes);
-  }
-  void give(Block& b) {
-    int dev = 0;
-    const bool other = cudaGetDevice(&dev) == cudaSuccess && dev != b.device && cudaSetDevice(b.device) == cudaSuccess;
-    const bool idle = cudaDeviceSynchronize() == cudaSuccess;
-    std::vector<void*> drop;
-    {
-      std::lock_guard<std::mutex> lock(mu_);
-      PerDevice& d = per_device_[b.device & 63];
-      --d.live;
-      if (idle) { d.free.emplace_back(b.ptr, b.bytes); d.kept += b.bytes; } else { drop.push_back(b.ptr); }
-      size_t n = 0;
-      while (n < d.free.size() && (d.live == 0 || d.kept > kKeep)) { drop.push_back(d.free[n].first); d.kept -= d.free[n].second; ++n; }
-      d.free.erase(d.free.begin(), d.free.begin() + static_cast<long>(n));
-    }
-    for (void* p : drop) cudaFree(p);
-    if (other) cudaSetDevice(dev);
-    b.ptr = nullptr;
-  }
-};
+EncodeTiledFn get_encode_fn() {
+  static EncodeTiledFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
+        qres == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiledFn>(p);
+  });
+  return fn;
+}
+
+bool chained_launches() { return g_hints.pdl != 0; }
+
+}  // namespace qc
 
 struct qgraph_inputs {
   qc::GraphInputRecord rec;
@@ -363,20 +271,6 @@ int place_weights(qconv_handle* h, DeviceParts& parts, const int8_t* w, size_t b
   }
   h->d_w = static_cast<int8_t*>(h->weights->ptr);
   return QCONV_OK;
-}
-
-// Multiplier and shift for the kernel's divisions by d (1 <= d < 2^31) of n < 2^31.  With 2^shr < d <= 2^(shr+1) and
-// mul = ceil(2^(32+shr) / d), e = mul d - 2^(32+shr) lies in [0, d), so n e < 2^31 2^(shr+1) = 2^(32+shr): the quotient
-// n mul / 2^(32+shr) exceeds n / d by less than 1 / d and has the same whole part.
-qc::FastDiv make_fastdiv(int d_in) {
-  qc::FastDiv f = {0u, 0u, static_cast<uint32_t>(std::max(1, d_in))};
-  if (f.d > 1u) {
-    uint32_t lg = 0;
-    while ((1ull << lg) < f.d) ++lg;                       // ceil(log2 d) >= 1
-    f.shr = lg - 1;
-    f.mul = static_cast<uint32_t>(((1ull << (32 + f.shr)) + f.d - 1) / f.d);
-  }
-  return f;
 }
 
 // Output-pixel box (tq x tp x tn <= 128) that wastes the fewest accumulator rows.
@@ -1579,22 +1473,6 @@ int prepare_dw_map(qconv_handle* h, const int8_t* x, int n_run, int channels, in
   return QCONV_OK;
 }
 
-// Launch with the programmatic-dependent-launch attribute (the kernel must call qc::chain_sync first).
-template <typename... KArgs, typename... Args>
-cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = g_hints.pdl != 0 ? 1 : 0;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
 // What the calling thread records between qgraph_record_begin and qgraph_record_end (NULL: nothing).
 thread_local std::unique_ptr<qc::GraphInputRecord> g_graph_inputs;
 
@@ -1606,11 +1484,6 @@ cudaError_t launch_input(void (*kernel)(KArgs...), dim3 grid, dim3 block, cudaSt
   if (e == cudaSuccess && g_graph_inputs)
     qc::note_graph_input(g_graph_inputs.get(), st, kernel, grid, block, size_t{0}, static_cast<KArgs>(args)...);
   return e;
-}
-
-int grid_for(size_t work_items, int threads, int max_blocks) {
-  size_t b = (work_items + threads - 1) / threads;
-  return static_cast<int>(std::max<size_t>(1, std::min<size_t>(b, max_blocks)));
 }
 
 }  // namespace
@@ -1633,6 +1506,10 @@ int qconv_checked_faults(int* first_line_out) {
     return fail(QCONV_ERR_CUDA, "qconv_checked_faults: cannot read the fault word");
   const int zero[2] = {0, 0};
   cudaMemcpyToSymbol(qc::g_checked_fault, zero, sizeof(zero));
+  int more[2] = {0, 0};                                    // of the other translation unit's kernels
+  if (qc::mx_checked_faults(more) != cudaSuccess) return fail(QCONV_ERR_CUDA, "qconv_checked_faults: cannot read the fault word");
+  if (v[0] == 0) v[1] = more[1];
+  v[0] += more[0];
 #else
   v[0] = -1;                                               // not a checked build
 #endif
