@@ -1,0 +1,263 @@
+// Products of microscaled 4-bit operands (kernel_mx_gemm.cuh has the mathematics, layouts and orientation) on PAIRS of SMs:
+// a cluster of two CTAs computes tiles of 256 output channels x 256 tokens with tcgen05.mma.cta_group::2.  Each CTA loads
+// the codes of its own 128 channels and of half the tokens, the scales of its channels and of all 256 tokens; per
+// multiply-add that is half the operand bytes of a 128 x 128 tile, which is what bounds long prompts.
+//
+// The kernel is persistent, and the epilogue of a tile runs beside the products of the next.  Two accumulators of 256
+// columns and the scales do not fit the 512 columns of tensor memory; the accumulators therefore overlap: tile i uses
+// columns 0 .. 255 or 208 .. 463 in turn, scales 464 .. 511.  The epilogue drains the shared 48 columns first and then
+// lets the next tile start; the rest of the tile is long drained when the tile after that one reaches it.
+//
+// Roles per CTA (320 threads): warp 0 lane 0 issues the loads, warp 1 owns tensor memory (lane 0 of the first CTA issues
+// scale copies and MMAs for both), warps 2-9 are the epilogue: tensor-memory lanes warp % 4, one half of the columns each.
+// Barriers as in kernel_igemm_pair.cuh: a stage's "full" lives in the first CTA and counts both CTAs' bytes; "empty" and
+// "accumulator full" arrive in both by multicast commits; "accumulator free" lives in the first CTA.  All waits are bounded.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+#include "kernel_igemm_pair.cuh"
+#include "kernel_mx_gemm.cuh"
+
+namespace qc {
+
+constexpr int kMxPairThreads = 64 + 32 * 8;
+constexpr int kMxPairStages = 5;
+constexpr int kMxPairTokens = 192;                                       // columns of a tile
+constexpr uint32_t kMxPairA = 128 * kMxStageBytes, kMxPairB = kMxPairTokens / 2 * kMxStageBytes;
+constexpr uint32_t kMxPairScaleB = 4 * kMxTileBytes;                     // of the 256 tokens whose scale tiles a tile touches
+constexpr uint32_t kMxPairStage = kMxPairA + kMxPairB + 2 * kMxTileBytes + kMxPairScaleB;
+constexpr int kMxPairScaleCol = 2 * kMxPairTokens, kMxPairScaleCols = 24;
+static_assert(kMxPairScaleCol + kMxPairStages * kMxPairScaleCols <= 512 && kMxPairStage % 1024 == 0);
+
+struct MxPairShared {
+  uint64_t full[kMxPairStages];
+  uint64_t empty[kMxPairStages];
+  uint64_t acc_full[2];
+  uint64_t acc_free[2];
+  uint64_t drained;
+  uint32_t tmem_base;
+  volatile int abort_flag;
+};
+constexpr size_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStage + sizeof(MxPairShared);
+
+namespace ptx {
+__device__ __forceinline__ void mma_mxf4_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem,
+                                              uint32_t sb_tmem, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate)
+      : "memory");
+}
+// Each CTA's scale tile at this shared-memory offset to its own tensor memory.
+__device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+}  // namespace ptx
+
+// Bounded wait with the hardware's suspend hint (one CTA an SM on long stages).
+__device__ __forceinline__ bool mx_wait_hint(uint32_t bar, uint32_t parity, unsigned int limit, volatile int* abort_flag, int* status) {
+  for (unsigned int it = 0; it < limit; ++it) {
+    if (ptx::mbar_try_wait_hint(bar, parity)) return true;
+    if (*abort_flag) return false;
+  }
+  *abort_flag = 1;
+  atomicExch(status, kStatusTimeout);
+  return false;
+}
+
+// Tile u of the walk: groups of eight token tiles, within a group channel tile after channel tile, so that pairs that run
+// side by side share both operands in L2.
+struct MxPairTile { int n0, t0; };
+__device__ __forceinline__ MxPairTile mx_pair_tile(const MxGemmParams& p, int u) {
+  const int per_group = 8 * p.tiles_n;
+  const int g = u / per_group, in = u - g * per_group;
+  const int wide = min(8, p.tiles_t - 8 * g);
+  const int tn = in / wide;
+  return {tn * 256, (8 * g + in - tn * wide) * kMxPairTokens};
+}
+
+template <typename Y>
+__global__ void __launch_bounds__(kMxPairThreads, 1)
+mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                    const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const MxGemmParams prm,
+                    const float* __restrict__ bias, Y* __restrict__ y, int* status, unsigned int wait_limit) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  MxPairShared* sh = reinterpret_cast<MxPairShared*>(ring + kMxPairStages * kMxPairStage);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int pair = static_cast<int>(blockIdx.x) >> 1, pairs = static_cast<int>(gridDim.x) >> 1;
+  const int total = prm.tiles_n * prm.tiles_t;
+  const uint32_t ring_addr = ptx::smem_u32(ring);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMxPairStages; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&sh->full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh->empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(ptx::smem_u32(&sh->acc_full[b]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh->acc_free[b]), 2 * 8);              // epilogue warps of both CTAs
+    }
+    ptx::mbar_init(ptx::smem_u32(&sh->drained), 1);
+    sh->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    ptx::fence_async_smem();
+    ptx::prefetch_tmap(&map_w);
+    ptx::prefetch_tmap(&map_x);
+    ptx::prefetch_tmap(&map_ws);
+    ptx::prefetch_tmap(&map_xs);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(ptx::smem_u32(&sh->tmem_base), 512);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync_all();                                   // the peer's barriers exist from here on
+  ptx::tc_fence_after();
+  const uint32_t tmem = sh->tmem_base;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+
+  // Both issuing warps run their loops with warp-uniform values, so that addresses, coordinates and descriptors live in
+  // uniform registers, where copies and MMAs take their operands from; one lane issues.
+  if (warp == 0) {
+    // ------------------------------------------------------------------ loads of this CTA's parts
+    const bool leader = ptx::elect_one();
+    bool ok = true;
+    int stage = 0;
+    uint32_t phase = 1;                                      // (the first pass over the ring finds every stage free)
+    const int peer_row = static_cast<int>(rank) * 128;
+    for (int u = pair; u < total && ok; u += pairs) {
+      const MxPairTile tile = mx_pair_tile(prm, u);
+      const int n0 = tile.n0 + peer_row, t0 = tile.t0 + static_cast<int>(rank) * (kMxPairTokens / 2);
+      for (int kb = 0; kb < prm.k_stages; ++kb) {
+        const uint32_t empty = ptx::smem_u32(&sh->empty[stage]);
+        if (!ptx::mbar_try_wait(empty, phase)) {
+          ok = mx_wait_hint(empty, phase, wait_limit, &sh->abort_flag, status);
+          if (!ok) break;
+        }
+        const uint32_t full = ptx::smem_u32(&sh->full[stage]), full0 = ptx::map_to_cta(full, 0u);
+        const uint32_t a = ring_addr + static_cast<uint32_t>(stage) * kMxPairStage;
+        if (leader) {
+          if (rank == 0) ptx::mbar_expect_tx(full, 2 * kMxPairStage);
+          ptx::tma_load_2d_pair(a, &map_w, full0, kb * kMxStageBytes, n0);
+          ptx::tma_load_2d_pair(a + kMxPairA, &map_x, full0, kb * kMxStageBytes, t0);
+          ptx::tma_load_2d_pair(a + kMxPairA + kMxPairB, &map_ws, full0, kb * 256, n0 >> 7);
+          ptx::tma_load_2d_pair(a + kMxPairA + kMxPairB + 2 * kMxTileBytes, &map_xs, full0, kb * 256, tile.t0 >> 7);
+        }
+        if (++stage == kMxPairStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    __syncwarp();
+    // after a wait that expired the copies on their way have time to land (microseconds; their barrier is the first CTA's)
+    if (leader && (!ok || sh->abort_flag))
+      for (int i = 0; i < 256; ++i) __nanosleep(200);
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      // ---------------------------------------------------------------- scales to tensor memory, products, for both CTAs
+      const bool leader = ptx::elect_one();
+      bool ok = true;
+      int stage = 0, tiles = 0;
+      uint32_t phase = 0;
+      const uint32_t idesc0 = make_idesc_mxf4(256, kMxPairTokens, 0), idesc1 = make_idesc_mxf4(256, kMxPairTokens, 1);
+      for (int u = pair; u < total && ok; u += pairs, ++tiles) {
+        const uint32_t acc = tmem + (tiles & 1 ? kMxPairTokens : 0);
+        // tokens of a tile may begin in the middle of a scale tile: 64 rows on are two columns on
+        const uint32_t sb_shift = (static_cast<uint32_t>(mx_pair_tile(prm, u).t0) >> 5) & 3u;
+        if (tiles > 1) {
+          ok = mx_wait_hint(ptx::smem_u32(&sh->acc_free[tiles & 1]), static_cast<uint32_t>((tiles >> 1) - 1) & 1u, wait_limit, &sh->abort_flag, status);
+          if (!ok) break;
+          ptx::tc_fence_after();
+        }
+        for (int kb = 0; kb < prm.k_stages; ++kb) {
+          const uint32_t full = ptx::smem_u32(&sh->full[stage]);
+          if (!ptx::mbar_try_wait(full, phase)) {
+            ok = mx_wait_hint(full, phase, wait_limit, &sh->abort_flag, status);
+            if (!ok) break;
+          }
+          ptx::tc_fence_after();
+          const uint32_t a = ring_addr + static_cast<uint32_t>(stage) * kMxPairStage;
+          const uint64_t sa_desc = make_scale_desc(a + kMxPairA + kMxPairB), sb_desc = sa_desc + (2 * kMxTileBytes >> 4);
+          const uint32_t sa = tmem + kMxPairScaleCol + static_cast<uint32_t>(stage) * kMxPairScaleCols, sb = sa + 8;
+          const uint64_t a_desc = make_kmajor_desc(a, kMxStageBytes), b_desc = make_kmajor_desc(a + kMxPairA, kMxStageBytes);
+          const bool both = prm.k_tiles - 2 * kb > 1;        // scale tiles of this stage: two but for an odd end
+          if (leader) {
+            ptx::tmem_copy_scales_pair(sa, sa_desc);
+            ptx::tmem_copy_scales_pair(sb, sb_desc);
+            ptx::tmem_copy_scales_pair(sb + 4, sb_desc + (2 * kMxTileBytes >> 4));
+            if (both) {
+              ptx::tmem_copy_scales_pair(sa + 4, sa_desc + (kMxTileBytes >> 4));
+              ptx::tmem_copy_scales_pair(sb + 8, sb_desc + (kMxTileBytes >> 4));
+              ptx::tmem_copy_scales_pair(sb + 12, sb_desc + (3 * kMxTileBytes >> 4));
+            }
+            ptx::mma_mxf4_pair(acc, a_desc, b_desc, idesc0, sa, sb + sb_shift, kb > 0);
+            ptx::mma_mxf4_pair(acc, a_desc + 2, b_desc + 2, idesc1, sa, sb + sb_shift, 1u);
+            if (both) {
+              ptx::mma_mxf4_pair(acc, a_desc + 4, b_desc + 4, idesc0, sa + 4, sb + 8 + sb_shift, 1u);
+              ptx::mma_mxf4_pair(acc, a_desc + 6, b_desc + 6, idesc1, sa + 4, sb + 8 + sb_shift, 1u);
+            }
+            ptx::mma_commit_pair(ptx::smem_u32(&sh->empty[stage]));
+          }
+          if (++stage == kMxPairStages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok && leader) ptx::mma_commit_pair(ptx::smem_u32(&sh->acc_full[tiles & 1]));
+      }
+      __syncwarp();
+      if (!ok && leader) {
+        // what was issued finishes before tensor memory and the operands go away
+        ptx::mma_commit_pair(ptx::smem_u32(&sh->drained));
+        for (unsigned int i = 0; i < kDrainPolls && !ptx::mbar_try_wait_hint(ptx::smem_u32(&sh->drained), 0u); ++i) {}
+      }
+    }
+    __syncwarp();
+  } else {
+    // -------------------------------------------------------------------- epilogue: lanes 32 (warp % 4) .., half the columns
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t free0 = ptx::map_to_cta(ptx::smem_u32(&sh->acc_free[0]), 0u);
+    int tiles = 0;
+    for (int u = pair; u < total; u += pairs, ++tiles) {
+      const MxPairTile tile = mx_pair_tile(prm, u);
+      const int n = tile.n0 + static_cast<int>(rank) * 128 + quad * 32 + lane;
+      const float b = bias != nullptr && n < prm.N ? __ldg(bias + n) : 0.0f;
+      const int buf = tiles & 1;
+      const bool ok = mx_wait_hint(ptx::smem_u32(&sh->acc_full[buf]), static_cast<uint32_t>(tiles >> 1) & 1u, wait_limit, &sh->abort_flag, status);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      ptx::tc_fence_after();
+      const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16) + (buf ? kMxPairTokens : 0);
+#pragma unroll 1
+      for (int c0 = half * (kMxPairTokens / 2); c0 < (half + 1) * (kMxPairTokens / 2); c0 += 32) {
+        uint32_t acc[32];
+        ptx::tmem_ld_32x32(lanes + c0, acc);
+        ptx::tmem_ld_wait();
+        Y* p = y + static_cast<size_t>(tile.t0 + c0) * prm.ld + n;
+        const int cols = n < prm.N ? prm.T - (tile.t0 + c0) : 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float v = __uint_as_float(acc[i]) + b;
+          if (prm.relu) v = v < 0.0f ? 0.0f : v;
+          if (i < cols) *p = from_float<Y>(v);
+          p += prm.ld;
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(free0 + 8u * static_cast<uint32_t>(buf));
+    }
+  }
+  // Nothing of this CTA goes away while the peer can still signal its barriers or multiply into its tensor memory.
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync_all();
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc_pair(tmem, 512);
+  }
+}
+
+}  // namespace qc

@@ -10,6 +10,7 @@
 
 #include "../../include/qconv.h"
 #include "kernel_mx_gemm.cuh"
+#include "kernel_mx_gemm_pair.cuh"
 #include "kernels_cache.cuh"
 #include "kernels_mx.cuh"
 #include "kernels_norm.cuh"
@@ -184,13 +185,13 @@ int encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, cuui
   return QCONV_OK;
 }
 // Codes [rows][K] in boxes of `box_rows` rows x 256 values, and their scale tiles in boxes of two tiles along the
-// contraction x box_rows / 128 (what a box reaches beyond the arrays is read as zeros).
-int encode_operand(CUtensorMap* codes, CUtensorMap* scales, const uint8_t* d_codes, const uint8_t* d_scales, int rows, int K, int box_rows) {
+// contraction x those of `scale_rows` rows (what a box reaches beyond the arrays is read as zeros).
+int encode_operand(CUtensorMap* codes, CUtensorMap* scales, const uint8_t* d_codes, const uint8_t* d_scales, int rows, int K, int box_rows, int scale_rows) {
   const cuuint64_t pitch = static_cast<cuuint64_t>(qc::mx_blocks(K)) * 16, tiles = qc::mx_tiles_k(K);
   int rc = encode_2d(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, d_codes, pitch, rows, pitch, qc::kMxStageBytes, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
   if (!rc)
     rc = encode_2d(scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, d_scales, tiles * 128, (rows + 127) / 128, tiles * qc::kMxTileBytes, 256,
-                   (box_rows + 127) / 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+                   (scale_rows + 127) / 128, CU_TENSOR_MAP_SWIZZLE_NONE);
   return rc;
 }
 
@@ -230,6 +231,34 @@ int launch_gemm(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   return QCONV_OK;
 }
 
+template <typename Y>
+cudaError_t allow_pair_smem() {
+  return cudaFuncSetAttribute(qc::mx_gemm_pair_kernel<Y>, cudaFuncAttributeMaxDynamicSharedMemorySize, qc::kMxPairSmem);
+}
+
+template <typename Y>
+int launch_pair(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
+  static qc::PerDevice<cudaError_t> allowed;
+  CUDA_TRY(allowed.once(h->device, allow_pair_smem<Y>));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2u * std::min(prm.tiles_n * prm.tiles_t, h->num_sms / 2));
+  cfg.blockDim = dim3(qc::kMxPairThreads);
+  cfg.dynamicSmemBytes = qc::kMxPairSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = qc::chained_launches() ? 1 : 0;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  h->bn = qc::kMxPairTokens; h->split = 0; h->stages = qc::kMxPairStages;
+  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_pair_kernel<Y>, h->map_w, h->map_x, h->map_ws, h->map_xs, prm, h->bias, y, h->d_status,
+                              h->wait_limit));
+  return QCONV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -247,7 +276,7 @@ int qmx_linear_create(qmx_linear** out, const qmx_linear_desc* desc, const uint8
   if (!h) return fail(QCONV_ERR_CUDA, "qmx_linear_create: out of host memory");
   h->d = *desc;
   h->w_codes = d_w_codes; h->w_scales = d_w_scales; h->bias = d_bias;
-  rc = encode_operand(&h->map_w, &h->map_ws, d_w_codes, d_w_scales, desc->N, desc->K, 128);
+  rc = encode_operand(&h->map_w, &h->map_ws, d_w_codes, d_w_scales, desc->N, desc->K, 128, 128);
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
   if (!rc && e == cudaSuccess) e = DevicePool::pool().take(&h->block, sizeof(int));
@@ -277,7 +306,10 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
   prm.k_tiles = qc::mx_tiles_k(d.K);
   prm.k_stages = (prm.k_tiles + 1) / 2;
   prm.tiles_n = (d.N + 127) / 128;
-  const int bn = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+  // pairs of SMs from about a wave of their tiles on
+  const bool pair = static_cast<long long>((d.N + 255) / 256) * ((tokens + 255) / 256) >= h->num_sms / 2;
+  const int bn = pair ? qc::kMxPairTokens : tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+  if (pair) prm.tiles_n = (d.N + 255) / 256;
   prm.tiles_t = (tokens + bn - 1) / bn;
   if (static_cast<long long>(prm.tiles_n) * prm.tiles_t > (1ll << 27)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "product too large");
   const int tiles = prm.tiles_n * prm.tiles_t;
@@ -285,7 +317,7 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
   while (prm.split < 8 && tiles * prm.split * 2 <= h->num_sms && prm.split * 2 <= prm.k_stages) prm.split *= 2;
   if (h->x_codes != d_x_codes || h->x_scales != d_x_scales || h->x_tokens != tokens || h->x_bn != bn) {
     h->x_codes = nullptr;
-    rc = encode_operand(&h->map_x, &h->map_xs, d_x_codes, d_x_scales, tokens, d.K, bn);
+    rc = encode_operand(&h->map_x, &h->map_xs, d_x_codes, d_x_scales, tokens, d.K, pair ? bn / 2 : bn, pair ? 256 : bn);
     if (rc) return rc;
     h->x_codes = d_x_codes; h->x_scales = d_x_scales; h->x_tokens = tokens; h->x_bn = bn;
   }
@@ -294,6 +326,7 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
   return with_type(d.type, [&](auto t) {
     using Y = decltype(t);
     Y* y = static_cast<Y*>(d_y);
+    if (pair) return launch_pair<Y>(h, prm, y, st);
     if (bn == 16) return launch_gemm<16, Y>(h, prm, y, st);
     if (bn == 32) return launch_gemm<32, Y>(h, prm, y, st);
     if (bn == 64) return launch_gemm<64, Y>(h, prm, y, st);
@@ -321,7 +354,8 @@ int qmx_linear_set_wait_limit(qmx_linear* h, unsigned int polls) {
 
 int qmx_linear_describe(const qmx_linear* h, char* buf, size_t buf_len) {
   if (!h || !buf || buf_len == 0) return fail(QCONV_ERR_BAD_ARG, "NULL argument");
-  snprintf(buf, buf_len, "mx N=%d K=%d tile=128x%d split=%d stages=%d", h->d.N, h->d.K, h->bn, h->split, h->stages);
+  snprintf(buf, buf_len, "mx N=%d K=%d tile=%dx%d split=%d pair=%d stages=%d", h->d.N, h->d.K, h->split == 0 ? 256 : 128, h->bn, std::max(1, h->split),
+           h->split == 0, h->stages);
   return QCONV_OK;
 }
 

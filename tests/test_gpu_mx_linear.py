@@ -54,6 +54,21 @@ def test_exact_sums(T, N, K, dtype):
     assert (flat == 77.0).all(), "written outside the output"
 
 
+@pytest.mark.parametrize("T,N,K", [(2048, 2560, 256), (2000, 2500, 1000), (1900, 4800, 130), (5000, 1100, 2050), (257, 19000, 96), (2600, 9999, 640)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_exact_sums_on_pairs_of_sms(T, N, K, dtype):
+    """Many tiles: several to a pair (both accumulators, the walk's groups) and ragged ends."""
+    import torch
+    rng = np.random.default_rng(T + N + K)
+    lin, xc, xs, _, x, w = layer(rng, T, N, K, dtype, bias=True, relu=True)
+    flat = torch.full((T * N + 64,), 77.0, dtype=lin.dtype, device="cuda")
+    y = lin.run(xc, xs, flat[:T * N].view(T, N))
+    assert lin.status() == 0 and "pair=1" in lin.describe()
+    want = torch.from_numpy(x).cuda() @ torch.from_numpy(w).cuda().T + lin._keep[2].double()
+    assert torch.equal(y, want.clamp(min=0).float().to(lin.dtype))
+    assert (flat[T * N:] == 77.0).all()
+
+
 @pytest.mark.parametrize("T,N,K", [(1, 300, 5000), (40, 200, 2000), (150, 300, 1024)])
 def test_real_operands(T, N, K):
     """Quantized normal values: scales of any size.  Every one of the sum's additions is off by at most 2^-23 of what is
