@@ -7,13 +7,12 @@
 //
 // A ring stage is 256 values of the contraction (128 bytes a row, the 128-byte swizzle): weight and token codes by TMA in
 // boxes of rows, their scales as tiles of 128 rows x 4 blocks (512 bytes; mx_format.cuh).  tcgen05.cp spreads a scale tile over
-// four columns of tensor memory; the four instructions of a stage take two scales a row each out of them.  The scales
-// have two places in tensor memory, and a stage's copies wait until the instructions that read the place
-// two stages before have finished.
+// four columns of tensor memory; the four instructions of a stage take two scales a row each out of them.  A ring
+// stage has its own place there, so that the barrier that frees the stage also says that its scales have been read.
 //
 // Roles (128 threads): warp 0 issues the loads, warp 1 owns tensor memory and issues copies and MMAs, then all four warps
-// drain a quarter of the lanes each.  With few tiles a cluster of CTAs shares a tile: each takes a part of the contraction,
-// leaves its sums in shared memory, and adds up its share of the columns over the cluster in a fixed order (no
+// drain a quarter of the lanes each.  With few tiles a cluster of CTAs shares a tile: each takes a part of the contraction
+// and sends its sums to the CTAs' shared memory, a share of the columns each, where they are added up in a fixed order (no
 // scratch in global memory, and the same result each time).  All waits are bounded.
 #pragma once
 #include <cuda.h>
@@ -36,7 +35,6 @@ struct MxGemmParams {
   int stages;                      // of the ring
   int split;                       // CTAs of a cluster that share a tile
   int relu;
-  uint32_t ring_bytes;             // of the ring, or of the sums that a cluster's CTAs leave in it if those need more
   size_t ld;                       // of y, in elements
 };
 
@@ -62,14 +60,14 @@ __device__ __forceinline__ void mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint6
 __device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+__device__ __forceinline__ float4 lds_float4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ void sts_f32(uint32_t addr, float v) {
-  asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
-}
+// The two halves of a cluster barrier.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 }  // namespace ptx
 
 // Shared-memory descriptor of a scale tile: 32 rows of 16 bytes, no swizzle, groups of eight rows 128 bytes apart.
@@ -108,15 +106,54 @@ __device__ __forceinline__ bool mx_wait(uint32_t bar, uint32_t parity, unsigned 
 
 template <int BN> struct MxTile {
   static constexpr uint32_t kA = 128 * kMxStageBytes, kB = BN * kMxStageBytes;
-  static constexpr int kTileAtomsB = (BN + 127) / 128;
-  static constexpr uint32_t kSA = 2 * kMxTileBytes, kSB = 2 * kTileAtomsB * kMxTileBytes;
+  static constexpr uint32_t kSA = 2 * kMxTileBytes, kSB = 2 * kMxTileBytes;
   static constexpr uint32_t kStage = kA + kB + kSA + kSB;              // a multiple of 1024
   static constexpr uint32_t kTx = kStage;
-  static constexpr int kScaleCols = 8 + 8 * kTileAtomsB;               // tensor-memory columns of a stage's scales
-  static constexpr int kUsedCols = BN + 2 * kScaleCols;
-  static constexpr int kCols = kUsedCols <= 64 ? 64 : kUsedCols <= 128 ? 128 : kUsedCols <= 256 ? 256 : 512;
-  static_assert(kUsedCols <= 512 && kStage % 1024 == 0);
+  static constexpr int kScaleCols = 16;                                // tensor-memory columns of a stage's scales
+  // 256 columns of tensor memory for two CTAs an SM, 128 where four may run
+  static constexpr int kCols = BN > 32 ? 256 : 128;
+  static constexpr int kMaxStages = (kCols - BN) / kScaleCols < kMxMaxStages ? (kCols - BN) / kScaleCols : kMxMaxStages;
+  static_assert(BN <= 128 && kMaxStages >= 2 && kStage % 1024 == 0);
 };
+
+// Columns that a warp drains at a time.
+template <int BN> constexpr int kMxChunk = BN < 32 ? 16 : 32;
+template <int BN>
+__device__ __forceinline__ void mx_drain(uint32_t taddr, uint32_t (&acc)[kMxChunk<BN>]) {
+  if constexpr (kMxChunk<BN> == 16) ptx::tmem_ld_32x16(taddr, acc); else ptx::tmem_ld_32x32(taddr, acc);
+  ptx::tmem_ld_wait();
+}
+
+// The sums of a tile shared by SPLIT CTAs (this one is number `part`; `cols` columns count, 0 after a failure).  Four columns
+// at a time belong to CTA group % SPLIT: everyone's 128 x 4 sums go to that CTA's shared memory, 16 bytes a lane, and
+// are added there in the order of the CTAs.  `done` gets each of this CTA's groups.
+template <int SPLIT, int BN, typename Done>
+__device__ __forceinline__ void mx_exchange(uint32_t lane_addr, uint32_t exchange_addr, int part, int cols, Done&& done) {
+  constexpr uint32_t kPlace = 128 * 16;                      // bytes of a CTA's sums of a group
+  const uint32_t mine = exchange_addr + threadIdx.x * 16;
+  uint32_t to[SPLIT];
+#pragma unroll
+  for (int p = 0; p < SPLIT; ++p) to[p] = ptx::map_to_cta(mine + static_cast<uint32_t>(part) * kPlace, static_cast<uint32_t>(p));
+  for (int c = 0; c < cols; c += kMxChunk<BN>) {             // (c / 4 is a multiple of SPLIT)
+    uint32_t acc[kMxChunk<BN>];
+    mx_drain<BN>(lane_addr + c, acc);
+#pragma unroll
+    for (int g = 0; g < kMxChunk<BN> / 4; ++g) {
+      const uint32_t place = static_cast<uint32_t>((c / 4 + g) / SPLIT * SPLIT) * kPlace;
+      if (c + 4 * g < cols) ptx::st_cluster_uint4(to[g % SPLIT] + place, acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
+    }
+  }
+  ptx::cluster_sync_all();
+  for (int g = part; 4 * g < cols; g += SPLIT) {
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int p = 0; p < SPLIT; ++p) {
+      const float4 w = ptx::lds_float4(mine + static_cast<uint32_t>(g / SPLIT * SPLIT + p) * kPlace);
+      v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+    }
+    done(4 * g, v);
+  }
+}
 
 template <int BN, typename Y>
 __global__ void __launch_bounds__(kMxGemmThreads)
@@ -126,8 +163,9 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   using Tile = MxTile<BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  MxGemmShared* sh = reinterpret_cast<MxGemmShared*>(ring + prm.ring_bytes);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  MxGemmShared* sh = reinterpret_cast<MxGemmShared*>(ring + static_cast<uint32_t>(prm.stages) * Tile::kStage);
+  const uint32_t exchange_addr = (ptx::smem_u32(sh + 1) + 15u) & ~15u;   // split > 1: 128 sums of each column, or of 4 split columns
+  const int warp = threadIdx.x >> 5;
   const int split = prm.split;
   const int part = split > 1 ? static_cast<int>(ptx::cluster_ctarank()) : 0;
   const int tile = static_cast<int>(blockIdx.x) / split;
@@ -160,74 +198,81 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = sh->tmem_base;
+  if (split > 1) ptx::cluster_arrive();
   ptx::grid_dependency_wait();                               // operands and y: other kernels' (the weights may be just written, too)
   ptx::grid_launch_dependents();
 
+  // Both issuing warps run their loops with warp-uniform values, so that addresses, coordinates and descriptors live in
+  // uniform registers, where copies and MMAs take their operands from; one lane issues.
   if (warp == 0) {
-    if (lane == 0) {
-      // ---------------------------------------------------------------- loads
-      bool ok = true;
-      int stage = 0, issued = 0;
-      uint32_t phase = 0;
-      for (int kb = kb0; kb < kb1 && ok; ++kb, ++issued) {
-        if (issued >= prm.stages) {
-          ok = mx_wait(ptx::smem_u32(&sh->empty[stage]), phase ^ 1u, wait_limit, &sh->abort_flag, status);
-          if (!ok) break;
-        }
-        const uint32_t bar = ptx::smem_u32(&sh->full[stage]);
-        const uint32_t a = ring_addr + static_cast<uint32_t>(stage) * Tile::kStage;
+    // ------------------------------------------------------------------ loads
+    const bool leader = ptx::elect_one();
+    bool ok = true;
+    int stage = 0, issued = 0;
+    uint32_t phase = 1;                                      // (the first pass over the ring finds every stage free)
+    for (int kb = kb0; kb < kb1; ++kb, ++issued) {
+      const uint32_t empty = ptx::smem_u32(&sh->empty[stage]);
+      if (wait_limit == 0u || !ptx::mbar_try_wait(empty, phase)) {
+        ok = mx_wait(empty, phase, wait_limit, &sh->abort_flag, status);
+        if (!ok) break;
+      }
+      const uint32_t bar = ptx::smem_u32(&sh->full[stage]);
+      const uint32_t a = ring_addr + static_cast<uint32_t>(stage) * Tile::kStage;
+      if (leader) {
         ptx::mbar_expect_tx(bar, Tile::kTx);
         ptx::tma_load_2d(a, &map_w, bar, kb * kMxStageBytes, n0);
         ptx::tma_load_2d(a + Tile::kA + Tile::kB, &map_ws, bar, kb * 256, tn);
         ptx::tma_load_2d(a + Tile::kA, &map_x, bar, kb * kMxStageBytes, t0);
         ptx::tma_load_2d(a + Tile::kA + Tile::kB + Tile::kSA, &map_xs, bar, kb * 256, t0 >> 7);
-        if (++stage == prm.stages) { stage = 0; phase ^= 1u; }
       }
-      if (!ok || sh->abort_flag) {
-        // the copies already issued land before this CTA's shared memory goes away (bounded, whatever the caller's limit)
-        for (int i = 0; i < issued && i < prm.stages; ++i) {
-          const int use = issued - 1 - i, s = use % prm.stages;
-          const uint32_t parity = static_cast<uint32_t>(use / prm.stages) & 1u;
-          for (unsigned int it = 0; it < kDrainPolls && !ptx::mbar_try_wait(ptx::smem_u32(&sh->full[s]), parity); ++it) {}
-        }
+      if (++stage == prm.stages) { stage = 0; phase ^= 1u; }
+    }
+    __syncwarp();
+    if (!ok || sh->abort_flag) {
+      // the copies already issued land before this CTA's shared memory goes away (bounded, whatever the caller's limit)
+      for (int i = 0; i < issued && i < prm.stages; ++i) {
+        const int use = issued - 1 - i, s = use % prm.stages;
+        const uint32_t parity = static_cast<uint32_t>(use / prm.stages) & 1u;
+        for (unsigned int it = 0; it < kDrainPolls && !ptx::mbar_try_wait(ptx::smem_u32(&sh->full[s]), parity); ++it) {}
       }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {
-      // ---------------------------------------------------------------- scales to tensor memory, products
-      bool ok = true;
-      int stage = 0;
-      uint32_t phase = 0;
-      const uint32_t idesc0 = make_idesc_mxf4(128, BN, 0), idesc1 = make_idesc_mxf4(128, BN, 1);
-      for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
-        ok = mx_wait(ptx::smem_u32(&sh->full[stage]), phase, wait_limit, &sh->abort_flag, status);
-        if (ok && it >= 2) {
-          // the instructions of two stages ago have read their scales out of the place that this stage's go to
-          const int use = it - 2, s = use % prm.stages;
-          ok = mx_wait(ptx::smem_u32(&sh->empty[s]), static_cast<uint32_t>(use / prm.stages) & 1u, wait_limit, &sh->abort_flag, status);
+    // ------------------------------------------------------------------ scales to tensor memory, products
+    const bool leader = ptx::elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    const uint32_t idesc0 = make_idesc_mxf4(128, BN, 0), idesc1 = make_idesc_mxf4(128, BN, 1);
+    for (int kb = kb0; kb < kb1; ++kb) {
+      const uint32_t full = ptx::smem_u32(&sh->full[stage]);
+      if (wait_limit == 0u || !ptx::mbar_try_wait(full, phase)) {
+        if (!mx_wait(full, phase, wait_limit, &sh->abort_flag, status)) break;
+      }
+      ptx::tc_fence_after();
+      const uint32_t a = ring_addr + static_cast<uint32_t>(stage) * Tile::kStage;
+      const uint64_t sa_desc = make_scale_desc(a + Tile::kA + Tile::kB), sb_desc = sa_desc + (Tile::kSA >> 4);
+      const uint32_t sa = tmem + BN + static_cast<uint32_t>(stage) * Tile::kScaleCols, sb = sa + 8;
+      const uint64_t a_desc = make_kmajor_desc(a, kMxStageBytes), b_desc = make_kmajor_desc(a + Tile::kA, kMxStageBytes);
+      const bool both = prm.k_tiles - 2 * kb > 1;            // scale tiles of this stage (128 values each): two but for an odd end
+      if (leader) {
+        ptx::tmem_copy_scales(sa, sa_desc);
+        ptx::tmem_copy_scales(sb, sb_desc);
+        if (both) {
+          ptx::tmem_copy_scales(sa + 4, sa_desc + (kMxTileBytes >> 4));
+          ptx::tmem_copy_scales(sb + 4, sb_desc + (kMxTileBytes >> 4));
         }
-        if (!ok) break;
-        ptx::tc_fence_after();
-        const uint32_t a = ring_addr + static_cast<uint32_t>(stage) * Tile::kStage;
-        const uint32_t sa_smem = a + Tile::kA + Tile::kB, sb_smem = sa_smem + Tile::kSA;
-        const uint32_t sa = tmem + BN + static_cast<uint32_t>(it & 1) * Tile::kScaleCols, sb = sa + 8;
-        const uint64_t a_desc = make_kmajor_desc(a, kMxStageBytes), b_desc = make_kmajor_desc(a + Tile::kA, kMxStageBytes);
-        const int halves = min(2, prm.k_tiles - 2 * kb);     // scale tiles of this stage: 128 values each
-        for (int k = 0; k < halves; ++k) {
-          ptx::tmem_copy_scales(sa + 4 * k, make_scale_desc(sa_smem + k * kMxTileBytes));
-#pragma unroll
-          for (int j = 0; j < Tile::kTileAtomsB; ++j)
-            ptx::tmem_copy_scales(sb + 4 * (k * Tile::kTileAtomsB + j), make_scale_desc(sb_smem + (2 * j + k) * kMxTileBytes));
-          const uint32_t sbk = sb + 4 * k * Tile::kTileAtomsB;
-          ptx::mma_mxf4(tmem, a_desc + 4 * k, b_desc + 4 * k, idesc0, sa + 4 * k, sbk, it > 0 || k > 0);
-          ptx::mma_mxf4(tmem, a_desc + 4 * k + 2, b_desc + 4 * k + 2, idesc1, sa + 4 * k, sbk, 1u);
+        ptx::mma_mxf4(tmem, a_desc, b_desc, idesc0, sa, sb, kb > kb0);
+        ptx::mma_mxf4(tmem, a_desc + 2, b_desc + 2, idesc1, sa, sb, 1u);
+        if (both) {
+          ptx::mma_mxf4(tmem, a_desc + 4, b_desc + 4, idesc0, sa + 4, sb + 4, 1u);
+          ptx::mma_mxf4(tmem, a_desc + 6, b_desc + 6, idesc1, sa + 4, sb + 4, 1u);
         }
         ptx::mma_commit(ptx::smem_u32(&sh->empty[stage]));
-        if (++stage == prm.stages) { stage = 0; phase ^= 1u; }
       }
-      ptx::mma_commit(ptx::smem_u32(&sh->acc_full));          // (after a wait that expired: of what was issued)
+      if (++stage == prm.stages) { stage = 0; phase ^= 1u; }
     }
+    __syncwarp();
+    if (leader) ptx::mma_commit(ptx::smem_u32(&sh->acc_full));            // (after a wait that expired: of what was issued)
     __syncwarp();
   }
   // -------------------------------------------------------------------- epilogue: warp w drains lanes 32 w .. 32 w + 31
@@ -246,36 +291,24 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     if (prm.relu) v = v < 0.0f ? 0.0f : v;
     if (t < prm.T && n < prm.N) y[static_cast<size_t>(t) * prm.ld + n] = from_float<Y>(v);
   };
-  constexpr int kChunk = BN < 32 ? 16 : 32;
   if (split == 1) {
     if (good)
-      for (int c = 0; c < BN && t0 + c < prm.T; c += kChunk) {
-        uint32_t acc[kChunk];
-        if constexpr (kChunk == 16) ptx::tmem_ld_32x16(lane_addr + c, acc); else ptx::tmem_ld_32x32(lane_addr + c, acc);
-        ptx::tmem_ld_wait();
+      for (int c = 0; c < BN && t0 + c < prm.T; c += kMxChunk<BN>) {
+        uint32_t acc[kMxChunk<BN>];
+        mx_drain<BN>(lane_addr + c, acc);
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) store(t0 + c + i, __uint_as_float(acc[i]));
+        for (int i = 0; i < kMxChunk<BN>; ++i) store(t0 + c + i, __uint_as_float(acc[i]));
       }
   } else {
-    // columns of 128 sums each, in the ring's memory: its loads and the instructions that read them are done
-    const int cols = min(BN, prm.T - t0);
-    if (good)
-      for (int c = 0; c < cols; c += kChunk) {
-        uint32_t acc[kChunk];
-        if constexpr (kChunk == 16) ptx::tmem_ld_32x16(lane_addr + c, acc); else ptx::tmem_ld_32x32(lane_addr + c, acc);
-        ptx::tmem_ld_wait();
+    ptx::cluster_wait();                                     // (the other CTAs run)
+    auto sums = [&](int c, float (&v)[4]) {
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i)
-          ptx::sts_f32(ring_addr + static_cast<uint32_t>((c + i) * 128 + threadIdx.x) * 4, __uint_as_float(acc[i]));
-      }
-    ptx::cluster_sync_all();
-    for (int c = part; c < cols; c += split) {
-      const uint32_t at = ring_addr + static_cast<uint32_t>(c * 128 + threadIdx.x) * 4;
-      float v = 0.0f;
-      for (int p = 0; p < split; ++p) v += ptx::ld_cluster_f32(ptx::map_to_cta(at, static_cast<uint32_t>(p)));
-      store(t0 + c, v);
-    }
-    ptx::cluster_sync_all();                                 // the others may still read this CTA's sums
+      for (int i = 0; i < 4; ++i) store(t0 + c + i, v[i]);
+    };
+    const int cols = good ? min(BN, prm.T - t0) : 0;
+    if (split == 2) mx_exchange<2, BN>(lane_addr, exchange_addr, part, cols, sums);
+    else if (split == 4) mx_exchange<4, BN>(lane_addr, exchange_addr, part, cols, sums);
+    else mx_exchange<8, BN>(lane_addr, exchange_addr, part, cols, sums);
   }
   ptx::tc_fence_before();
   __syncthreads();

@@ -137,7 +137,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
       const int n0 = tile.n0 + peer_row, t0 = tile.t0 + static_cast<int>(rank) * (kMxPairTokens / 2);
       for (int kb = 0; kb < prm.k_stages; ++kb) {
         const uint32_t empty = ptx::smem_u32(&sh->empty[stage]);
-        if (!ptx::mbar_try_wait(empty, phase)) {
+        if (wait_limit == 0u || !ptx::mbar_try_wait(empty, phase)) {
           ok = mx_wait_hint(empty, phase, wait_limit, &sh->abort_flag, status);
           if (!ok) break;
         }
@@ -177,7 +177,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         }
         for (int kb = 0; kb < prm.k_stages; ++kb) {
           const uint32_t full = ptx::smem_u32(&sh->full[stage]);
-          if (!ptx::mbar_try_wait(full, phase)) {
+          if (wait_limit == 0u || !ptx::mbar_try_wait(full, phase)) {
             ok = mx_wait_hint(full, phase, wait_limit, &sh->abort_flag, status);
             if (!ok) break;
           }

@@ -206,12 +206,15 @@ int launch_gemm(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   static qc::PerDevice<cudaError_t> allowed;
   CUDA_TRY(allowed.once(h->device, allow_gemm_smem<BN, Y>));
   const int per_cta = (prm.k_stages + prm.split - 1) / prm.split;
-  // two CTAs an SM where their columns of tensor memory and a ring worth having fit, so that one drains while the other multiplies
-  const uint32_t room = (Tile::kCols <= 256 ? 113u : 227u) * 1024 - 1024 - sizeof(qc::MxGemmShared);
-  prm.stages = std::max(2, std::min({per_cta, static_cast<int>(room / Tile::kStage), qc::kMxMaxStages}));
-  prm.ring_bytes = prm.stages * Tile::kStage;
-  if (prm.split > 1) prm.ring_bytes = std::max<uint32_t>(prm.ring_bytes, BN * 512);
-  const size_t smem = 1024 + prm.ring_bytes + sizeof(qc::MxGemmShared);
+  // Two CTAs an SM, so that one drains (or sets up, in the next launch) while the other multiplies; a deeper ring instead where
+  // every CTA has an SM to itself and walks a long part of the contraction on wide stages (us with half an SM's memory / all of
+  // it: 48 tokens x 16384 x 8192 17.3 / 16.0, 128 x 8192 x 8192 16.5 / 13.6; the other way round 64 x 4096 x 4096, four stages
+  // a CTA, 5.3 / 6.0).  A shared tile's sums have shared memory of their own.
+  const uint32_t sums = prm.split > 1 ? 16 + std::max(BN, 4 * prm.split) * 512 : 0;
+  const bool alone = prm.tiles_n * prm.tiles_t * prm.split <= h->num_sms && BN >= 64 && per_cta >= 8;
+  const uint32_t room = (alone ? 227u : 113u) * 1024 - 1024 - sizeof(qc::MxGemmShared) - sums;
+  prm.stages = std::max(2, std::min({per_cta, static_cast<int>(room / Tile::kStage), Tile::kMaxStages}));
+  const size_t smem = 1024 + static_cast<size_t>(prm.stages) * Tile::kStage + sizeof(qc::MxGemmShared) + sums;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned int>(prm.tiles_n) * prm.tiles_t * prm.split);
   cfg.blockDim = dim3(qc::kMxGemmThreads);
@@ -306,15 +309,22 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
   prm.k_tiles = qc::mx_tiles_k(d.K);
   prm.k_stages = (prm.k_tiles + 1) / 2;
   prm.tiles_n = (d.N + 127) / 128;
-  // pairs of SMs from about a wave of their tiles on
-  const bool pair = static_cast<long long>((d.N + 255) / 256) * ((tokens + 255) / 256) >= h->num_sms / 2;
-  const int bn = pair ? qc::kMxPairTokens : tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+  const int bn_one = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+  const long long tiles_one = static_cast<long long>((d.N + 127) / 128) * ((tokens + bn_one - 1) / bn_one);
+  const long long tiles_pair = static_cast<long long>((d.N + 255) / 256) * ((tokens + qc::kMxPairTokens - 1) / qc::kMxPairTokens);
+  if (tiles_one > (1ll << 27)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "product too large");
+  prm.split = 1;
+  while (prm.split < 8 && tiles_one * prm.split * 2 <= h->num_sms && prm.split * 2 <= prm.k_stages) prm.split *= 2;
+  // Tiles on pairs of SMs take about 0.36 us a stage and wave, those of single SMs 0.5 us, and sharing a tile 2 us more (us,
+  // single / pair: 128 tokens x 8192 x 8192 13.6 / 14.6, 256 x 4096 x 4096 9.2 / 8.4, 512 x 4096 x 4096 11.8 / 9.0, 256 x 8192 x
+  // 8192 20.1 / 14.9, 1024 x 2048 x 4096 10.8 / 8.7); up to 64 tokens a pair's columns are mostly empty.
+  const int wave_pair = h->num_sms / 2;
+  const double us_pair = 0.36 * prm.k_stages * ((tiles_pair + wave_pair - 1) / wave_pair);
+  const double us_one = 0.5 * ((prm.k_stages + prm.split - 1) / prm.split) * ((tiles_one * prm.split + h->num_sms - 1) / h->num_sms) + (prm.split > 1 ? 2.0 : 0.0);
+  const bool pair = tokens > 64 && us_pair <= us_one;
+  const int bn = pair ? qc::kMxPairTokens : bn_one;
   if (pair) prm.tiles_n = (d.N + 255) / 256;
   prm.tiles_t = (tokens + bn - 1) / bn;
-  if (static_cast<long long>(prm.tiles_n) * prm.tiles_t > (1ll << 27)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "product too large");
-  const int tiles = prm.tiles_n * prm.tiles_t;
-  prm.split = 1;
-  while (prm.split < 8 && tiles * prm.split * 2 <= h->num_sms && prm.split * 2 <= prm.k_stages) prm.split *= 2;
   if (h->x_codes != d_x_codes || h->x_scales != d_x_scales || h->x_tokens != tokens || h->x_bn != bn) {
     h->x_codes = nullptr;
     rc = encode_operand(&h->map_x, &h->map_xs, d_x_codes, d_x_scales, tokens, d.K, pair ? bn / 2 : bn, pair ? 256 : bn);

@@ -9,7 +9,9 @@ pytestmark = pytest.mark.gpu
 
 # (tokens, N, K): every column width, one to many tiles, split and whole contractions, ragged everything
 SHAPES = [(1, 1, 1), (1, 128, 256), (3, 130, 33), (16, 256, 512), (17, 384, 1000), (33, 64, 4096), (64, 1024, 2048), (65, 100, 130),
-          (128, 640, 257), (129, 200, 300), (300, 513, 700), (1, 4096, 4096), (8, 20000, 320), (200, 2100, 4100)]
+          (128, 640, 257), (129, 200, 300), (300, 513, 700), (1, 4096, 4096), (8, 20000, 320), (200, 2100, 4100),
+          # (on single SMs: few tiles and a long contraction, shared by eight, four, two; rings that go round many times)
+          (256, 256, 6000), (130, 500, 7000), (100, 8000, 4000), (70, 16000, 1100), (40, 19000, 2500)]
 
 
 def operand(rng, rows, K, low=126, high=129):
