@@ -1,7 +1,8 @@
 // Quantized caches: the values of a token's heads are converted as they are written to their slot, and read back from
 // any list of slots.  A head's D values are one group: int8 with an exponent for the group, or microscaled 4 bits.  Bound by
-// HBM on long lists and by the launch on short ones: keys and values go in one launch, a head takes 8, 16 or 32 lanes
-// with eight values a lane (several times over where D > 256).
+// HBM on long lists and by the launch on short ones: keys and values go in one launch, a head takes LANES lanes with V
+// pieces of 32 bytes each, and a group of lanes has kCacheUnroll heads in flight (their slots, codes and scales are a chain
+// of dependent loads).
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
@@ -10,6 +11,18 @@ namespace qc {
 
 enum : int { CACHE_I8 = 0, CACHE_MX = 1 };
 constexpr int kCacheThreads = 256;
+#ifndef CWU
+#define CWU 2
+#endif
+#ifndef CRU
+#define CRU 4
+#endif
+#ifndef CWB
+#define CWB 4
+#endif
+#ifndef CRB
+#define CRB 4
+#endif
 
 struct CacheSide {
   uint8_t* codes;
@@ -25,148 +38,179 @@ struct CacheArgs {
   int items;                 // rows * sides * heads, below 2^30
   FastDiv fd_heads;
   int sides;
-  int vec_ok, code_vec;      // eight values / eight int8 codes are aligned
+  int how, code_vec;         // ROWS_* of the values; a lane's int8 codes are aligned
   int code_pitch, scale_pitch;   // bytes of a head's codes and scales
 };
 
 struct CacheItem {
-  int side;
-  bool valid;
+  bool valid, second;        // second: of the values, not the keys
   size_t values, group;      // element offset of the head's values; index of (slot, head)
 };
 __device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, int u) {
-  CacheItem c = {0, false, 0, 0};
+  CacheItem c = {false, false, 0, 0};
   if (u >= a.items) return c;
   int h;
   const int rs = a.fd_heads.divmod(u, &h);
   const int row = a.sides == 2 ? rs >> 1 : rs;
-  c.side = a.sides == 2 ? rs & 1 : 0;
+  c.second = a.sides == 2 && (rs & 1);
   const long long slot = __ldg(a.slots + row);
-  c.valid = slot >= 0 && slot < a.num_slots;
-  const CacheSide& s = a.side[c.side];
-  c.values = static_cast<size_t>(row * s.token + h * s.head);
+  c.valid = slot >= 0 && slot < a.num_slots && QC_IN(slot, a.num_slots);
+  c.values = static_cast<size_t>(row * (c.second ? a.side[1].token : a.side[0].token) + h * (c.second ? a.side[1].head : a.side[0].head));
   c.group = static_cast<size_t>(slot) * a.heads + h;
   return c;
 }
+__device__ __forceinline__ uint8_t* cache_codes(const CacheArgs& a, const CacheItem& c) {
+  return (c.second ? a.side[1].codes : a.side[0].codes) + c.group * a.code_pitch;
+}
+__device__ __forceinline__ uint8_t* cache_scales(const CacheArgs& a, const CacheItem& c) {
+  return (c.second ? a.side[1].scales : a.side[0].scales) + c.group * a.scale_pitch;
+}
+template <typename T>
+__device__ __forceinline__ T* cache_values(const CacheArgs& a, const CacheItem& c) {
+  return static_cast<T*>(c.second ? a.side[1].values : a.side[0].values) + c.values;
+}
 
-// LANES lanes a head, V vectors of eight values a lane.
-template <typename T, int FMT, int LANES, int V>
-__global__ void __launch_bounds__(kCacheThreads)
+// LANES lanes a head, V pieces a lane.
+template <typename T, int FMT, int LANES, int V, bool ANY>
+__global__ void __launch_bounds__(kCacheThreads, V == 1 ? CWB : 1)
 cache_write_kernel(const CacheArgs a) {
+  constexpr int E = Piece<T>::E, U = V == 1 ? CWU : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
+  __shared__ uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  constexpr int kPerBlock = kCacheThreads / LANES;
   const int lane = threadIdx.x & (LANES - 1);
   const int step = gridDim.x * kPerBlock;
+  uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
   // the lanes of a warp run the same number of rounds
-  const int mine = threadIdx.x / LANES, warp_first = (threadIdx.x & ~31) / LANES;
-  for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += step) {
-    const CacheItem c = cache_item(a, base + mine - warp_first);
-    const CacheSide& s = a.side[c.side];
-    const T* x = static_cast<const T*>(s.values) + c.values;
-    float v[V][8];
+  const int warp_first = (threadIdx.x >> 5) * kPerWarp, mine = (threadIdx.x & 31) / LANES;
+  for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += U * step) {
+    CacheItem c[U];
+    Piece<T> x[U][V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const int col = (k * LANES + lane) * 8, n = a.D - col;
-      if (c.valid && n >= 8 && a.vec_ok) {
-        Eight<T> e;
-        e.load(x + col);
-        e.unpack(v[k]);
+    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine);
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        group_load<ANY>(x[j][k], cache_values<T>(a, c[j]) + k * LANES * E, c[j].valid ? a.D - k * LANES * E : 0, LANES, lane, a.how, stage);
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      uint8_t* codes = cache_codes(a, c[j]);
+      uint8_t* scales = cache_scales(a, c[j]);
+      if constexpr (FMT == CACHE_I8) {
+        float v[V][E];
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          x[j][k].unpack(v[k]);
+          m = max(m, finite_top<1>(v[k], x[j][k].top()));
+        }
+        const uint32_t sb = i8_scale_byte(max_over<LANES>(m));
+        const float inv = inverse_scale(sb);
+        if (c[j].valid && lane == 0) *scales = static_cast<uint8_t>(sb);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const int col = (k * LANES + lane) * E, n = min(E, a.D - col);
+          uint32_t w[E / 4];
+#pragma unroll
+          for (int i = 0; i < E / 4; ++i) w[i] = i8_encode_four(v[k] + 4 * i, inv);
+          if (!c[j].valid || n <= 0) continue;
+          if (a.code_vec) {
+            if constexpr (E == 8) *reinterpret_cast<uint2*>(codes + col) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint4*>(codes + col) = make_uint4(w[0], w[1], w[2], w[3]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+              if (i < n) codes[col + i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i & 3)));
+          }
+        }
       } else {
-        load_some(x + col, c.valid ? n : 0, v[k]);
-      }
-    }
-    uint8_t* codes = s.codes + c.group * a.code_pitch;
-    uint8_t* scales = s.scales + c.group * a.scale_pitch;
-    const bool in = c.valid && QC_IN(c.group, static_cast<size_t>(a.num_slots) * a.heads);
-    if constexpr (FMT == CACHE_I8) {
-      uint32_t m = 0;
+        constexpr int kBlockLanes = kMxBlock / E;
 #pragma unroll
-      for (int k = 0; k < V; ++k) m = max(m, finite_top<1>(v[k]));
-      const uint32_t sb = i8_scale_byte(max_over<LANES>(m));
-      if (in && lane == 0) *scales = static_cast<uint8_t>(sb);
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const int col = (k * LANES + lane) * 8, n = min(8, a.D - col);
-        if (!in || n <= 0) continue;
-        const uint2 w = i8_encode_eight(v[k], inverse_scale(sb));
-        if (n == 8 && a.code_vec) *reinterpret_cast<uint2*>(codes + col) = w;
-        else
-          for (int i = 0; i < n; ++i) codes[col + i] = static_cast<uint8_t>((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const int col = (k * LANES + lane) * 8;
-        const uint32_t sb = mx_scale_byte(finite_top<4>(v[k]), 0x3FFFFFu);
-        if (!in || col >= a.blocks * kMxBlock) continue;
-        *reinterpret_cast<uint32_t*>(codes + col / 2) = mx_encode_eight(v[k], inverse_scale(sb));
-        if ((col & 31) == 0) scales[col / kMxBlock] = static_cast<uint8_t>(sb);
+        for (int k = 0; k < V; ++k) {
+          const int col = (k * LANES + lane) * E;
+          float v[E];
+          x[j][k].unpack(v);
+          const uint32_t sb = mx_scale_byte(finite_top<kBlockLanes>(v, x[j][k].top()), kCoverRoundUp);
+          if (!c[j].valid || col >= a.blocks * kMxBlock) continue;
+          mx_store_codes(codes + col / 2, v, inverse_scale(sb));
+          if ((col & (kMxBlock - 1)) == 0) scales[col / kMxBlock] = static_cast<uint8_t>(sb);
+        }
       }
     }
   }
 }
 
-constexpr int kCacheUnroll = 4;                 // heads a group of lanes has in flight on the way back
-
-template <typename T, int FMT, int LANES, int V>
-__global__ void __launch_bounds__(kCacheThreads)
+template <typename T, int FMT, int LANES, int V, bool ANY>
+__global__ void __launch_bounds__(kCacheThreads, V == 1 ? CRB : 1)
 cache_read_kernel(const CacheArgs a) {
+  constexpr int E = Piece<T>::E, U = V == 1 ? CRU : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
+  __shared__ uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  constexpr int kPerBlock = kCacheThreads / LANES;
-  constexpr int U = V == 1 ? kCacheUnroll : 1;
   const int lane = threadIdx.x & (LANES - 1);
   const int step = gridDim.x * kPerBlock;
-  for (int base = blockIdx.x * kPerBlock + threadIdx.x / LANES; base < a.items; base += U * step) {
+  uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
+  const int warp_first = (threadIdx.x >> 5) * kPerWarp, mine = (threadIdx.x & 31) / LANES;
+  for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += U * step) {
     CacheItem c[U];
-    uint2 w[U][V];
-    uint32_t sb[U][V];
+    uint32_t w[U][V][E / 4], sb[U][V];                      // (4-bit codes: the first half)
 #pragma unroll
-    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step);
+    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const uint8_t* codes = a.side[c[j].side].codes + c[j].group * a.code_pitch;
-      const uint8_t* scales = a.side[c[j].side].scales + c[j].group * a.scale_pitch;
-      const bool in = c[j].valid && QC_IN(c[j].group, static_cast<size_t>(a.num_slots) * a.heads);
+      const uint8_t* codes = cache_codes(a, c[j]);
+      const uint8_t* scales = cache_scales(a, c[j]);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const int col = (k * LANES + lane) * 8, n = min(8, a.D - col);
-        w[j][k] = make_uint2(0u, 0u);
+        const int col = (k * LANES + lane) * E, n = c[j].valid ? min(E, a.D - col) : 0;
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) w[j][k][i] = 0u;
         sb[j][k] = kScaleOne;
-        if (!in || n <= 0) continue;
+        if (n <= 0) continue;
         if constexpr (FMT == CACHE_I8) {
           sb[j][k] = __ldg(scales);
-          if (n == 8 && a.code_vec) w[j][k] = __ldg(reinterpret_cast<const uint2*>(codes + col));
-          else
-            for (int i = 0; i < n; ++i) {
-              const uint32_t b = static_cast<uint32_t>(__ldg(codes + col + i)) << (8 * (i & 3));
-              if (i < 4) w[j][k].x |= b; else w[j][k].y |= b;
+          if (a.code_vec) {
+            if constexpr (E == 8) {
+              const uint2 q = __ldg(reinterpret_cast<const uint2*>(codes + col));
+              w[j][k][0] = q.x; w[j][k][1] = q.y;
+            } else {
+              const uint4 q = __ldg(reinterpret_cast<const uint4*>(codes + col));
+              w[j][k][0] = q.x; w[j][k][1] = q.y; w[j][k][2] = q.z; w[j][k][3] = q.w;
             }
+          } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+              if (i < n) w[j][k][i / 4] |= static_cast<uint32_t>(__ldg(codes + col + i)) << (8 * (i & 3));
+          }
         } else {
           sb[j][k] = __ldg(scales + col / kMxBlock);
-          w[j][k].x = __ldg(reinterpret_cast<const uint32_t*>(codes + col / 2));
+          if constexpr (E == 8) {
+            w[j][k][0] = __ldg(reinterpret_cast<const uint32_t*>(codes + col / 2));
+          } else {
+            const uint2 q = __ldg(reinterpret_cast<const uint2*>(codes + col / 2));
+            w[j][k][0] = q.x; w[j][k][1] = q.y;
+          }
         }
       }
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      if (!c[j].valid) continue;
-      T* y = static_cast<T*>(a.side[c[j].side].values) + c[j].values;
+      T* y = cache_values<T>(a, c[j]);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const int col = (k * LANES + lane) * 8, n = a.D - col;
-        if (n <= 0) continue;
-        float v[8];
-        if constexpr (FMT == CACHE_I8) i8_decode_eight(w[j][k], scale_of(sb[j][k]), v);
-        else mx_decode_eight(w[j][k].x, scale_of(sb[j][k]), v);
-        if (n >= 8 && a.vec_ok) {
-          Eight<T> e;
-          e.pack(v);
-          e.store(y + col);
+        float v[E];
+        const float scale = scale_of(sb[j][k]);
+        if constexpr (FMT == CACHE_I8) {
+#pragma unroll
+          for (int i = 0; i < E / 4; ++i) i8_decode_four(w[j][k][i], scale, v + 4 * i);
         } else {
-          store_some(y + col, n, v);
+#pragma unroll
+          for (int i = 0; i < E / 8; ++i) mx_decode_eight(w[j][k][i], scale, v + 8 * i);
         }
+        Piece<T> p;
+        p.pack(v);
+        group_store<ANY>(p, y + k * LANES * E, c[j].valid ? a.D - k * LANES * E : 0, LANES, lane, a.how, stage);
       }
     }
   }

@@ -1,6 +1,7 @@
 // Tensors to microscaled 4-bit codes and back (mx_format.cuh has the type).  Both directions are bound by HBM: 2 or 4
-// bytes in and 17/32 out per value, or the other way round.  Sixteen lanes take 128 consecutive values of a row, eight
-// each (16-byte accesses): a block is four lanes, its maximum two shuffles, and the four scales of the sixteen lanes are one word.
+// bytes in and 17/32 out per value, or the other way round.  A lane takes 32 bytes of values, so that a block is two or
+// four lanes (its maximum one or two shuffles) and the scales of eight or sixteen lanes are one word.  A thread stays in its
+// columns and walks down the rows, kMxUnroll of them at a time, so that an address is one product and no division is left.
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
@@ -8,99 +9,104 @@
 namespace qc {
 
 constexpr int kMxThreads = 256;
-constexpr int kMxUnroll = 4;                    // pieces of 128 values a half-warp has in flight
+// Rows a thread has in flight.
+#ifndef MXU
+#define MXU 1
+#endif
+#ifndef MXB
+#define MXB 6
+#endif
+constexpr int kMxUnroll = MXU;
 
-// Units: 128-value piece g of row r, r slowest.  In tiles the rows up to the next multiple of 128 have units too, which
-// write their scale words (2^0) alone.
-template <typename T>
-__global__ void __launch_bounds__(kMxThreads)
-mx_quantize_kernel(const T* __restrict__ x, size_t ld, size_t rows, int K, uint8_t* __restrict__ codes, MxScales scales, uint32_t round_up,
-                   int units, FastDiv fd_pieces, int vec_ok) {
+// A block is lanes_x lanes (a power of two, at least those of a scale word) along the row by kMxThreads / lanes_x rows.
+struct MxGrid {
+  int lanes_x, log_x;
+  size_t rows;            // of the tensor
+  size_t rows_out;        // with the rows that fill up the last tile (quantisation into tiles)
+  int K;
+  size_t ld;
+  int how;                // ROWS_*
+};
+
+template <typename T, bool ANY>
+__global__ void __launch_bounds__(kMxThreads, MXB)
+mx_quantize_kernel(const T* __restrict__ x, const MxGrid g, uint8_t* __restrict__ codes, const MxScales scales, uint32_t round_up) {
+  constexpr int E = Piece<T>::E, kBlockLanes = kMxBlock / E, kWordLanes = 4 * kBlockLanes;
+  __shared__ uint8_t stage[ANY ? kMxThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int lane16 = threadIdx.x & 15;
-  const int halves = gridDim.x * (kMxThreads / 16);
-  const size_t code_pitch = static_cast<size_t>(scales.blocks) * 16;
-  // both halves of a warp run the same number of rounds
-  const int first = blockIdx.x * (kMxThreads / 16) + (threadIdx.x >> 4), first_even = first & ~1;
-  for (int base = first_even; base < units; base += halves * kMxUnroll) {
-    float v[kMxUnroll][8];
+  const int G = min(g.lanes_x, 32);
+  const int lane_x = threadIdx.x & (g.lanes_x - 1), lane = lane_x & (G - 1);
+  const int col = (static_cast<int>(blockIdx.x) * g.lanes_x + lane_x) * E, first = col - lane * E;   // of the lane, of its group
+  const size_t pitch = static_cast<size_t>(scales.blocks) * 16;
+  const size_t step = static_cast<size_t>(gridDim.y) * (kMxThreads >> g.log_x);
+  const bool codes_here = col < scales.blocks * kMxBlock;
+  const bool word_here = codes_here && (lane_x & (kWordLanes - 1)) == 0;
+  uint8_t* my_stage = stage[ANY ? threadIdx.x >> 5 : 0];
+  // every lane of a warp goes round as often as the warp's first
+  const size_t warp_row = (threadIdx.x & ~31u) >> g.log_x, my_row = (threadIdx.x >> g.log_x) - warp_row;
+  for (size_t base = blockIdx.y * static_cast<size_t>(kMxThreads >> g.log_x) + warp_row; base < g.rows_out; base += kMxUnroll * step) {
+    Piece<T> p[kMxUnroll];
 #pragma unroll
     for (int j = 0; j < kMxUnroll; ++j) {
-      const int u = base + (first & 1) + j * halves;
-      int g = 0;
-      const size_t r = u < units ? fd_pieces.divmod(u, &g) : rows;
-      const int col = g * 128 + lane16 * 8, n = K - col;
-      const T* p = x + r * ld + col;
-      if (r < rows && n >= 8 && vec_ok && QC_IN(r * ld + col + 7, (rows - 1) * ld + K)) {
-        Eight<T> e;
-        e.load(p);
-        e.unpack(v[j]);
-      } else if (r < rows && n > 0 && QC_IN(r * ld + col + min(n, 8) - 1, (rows - 1) * ld + K)) {
-        load_some(p, n, v[j]);
-      } else {
-        load_some(p, 0, v[j]);
-      }
+      const size_t r = base + j * step + my_row;
+      const int n = r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0;
+      group_load<ANY>(p[j], x + r * g.ld + first, n, G, lane, g.how, my_stage);
     }
 #pragma unroll
     for (int j = 0; j < kMxUnroll; ++j) {
-      const int u = base + (first & 1) + j * halves;
-      if (base + j * halves >= units) break;                // (the same for the whole warp: base is even)
-      int g = 0;
-      const size_t r = u < units ? fd_pieces.divmod(u, &g) : rows;
-      const uint32_t s = mx_scale_byte(finite_top<4>(v[j]), round_up);
-      const uint32_t word = gather_scale_word(s);
-      const int at = g * 64 + lane16 * 4;                   // byte of the row's codes
-      if (r < rows && at < scales.blocks * 16 && QC_IN(r * code_pitch + at + 3, rows * code_pitch))
-        *reinterpret_cast<uint32_t*>(codes + r * code_pitch + at) = mx_encode_eight(v[j], inverse_scale(s));
-      if (lane16 == 0 && u < units) store_scale_word(scales, r, g, word);
+      const size_t r = base + j * step + my_row;
+      float v[E];
+      p[j].unpack(v);
+      const uint32_t s = mx_scale_byte(finite_top<kBlockLanes>(v, p[j].top()), round_up);
+      const uint32_t word = gather_scale_word<kBlockLanes>(s);
+      if (codes_here && r < g.rows && QC_IN(r * pitch + col / 2 + E / 2 - 1, g.rows * pitch))
+        mx_store_codes(codes + r * pitch + col / 2, v, inverse_scale(s));
+      if (word_here && r < g.rows_out) store_scale_word(scales, r, col >> 7, word);
     }
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kMxThreads)
-mx_dequantize_kernel(const uint8_t* __restrict__ codes, MxScales scales, size_t rows, int K, T* __restrict__ y, size_t ld, int units,
-                     FastDiv fd_pieces, int vec_ok) {
+template <typename T, bool ANY>
+__global__ void __launch_bounds__(kMxThreads, MXB)
+mx_dequantize_kernel(const uint8_t* __restrict__ codes, const MxScales scales, const MxGrid g, T* __restrict__ y) {
+  constexpr int E = Piece<T>::E;
+  __shared__ uint8_t stage[ANY ? kMxThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int lane16 = threadIdx.x & 15;
-  const int halves = gridDim.x * (kMxThreads / 16);
-  const size_t code_pitch = static_cast<size_t>(scales.blocks) * 16;
-  for (int base = blockIdx.x * (kMxThreads / 16) + (threadIdx.x >> 4); base < units; base += halves * kMxUnroll) {
-    uint32_t w[kMxUnroll], s[kMxUnroll];
+  const int G = min(g.lanes_x, 32);
+  const int lane_x = threadIdx.x & (g.lanes_x - 1), lane = lane_x & (G - 1);
+  const int col = (static_cast<int>(blockIdx.x) * g.lanes_x + lane_x) * E, first = col - lane * E;
+  const int b = col / kMxBlock;
+  const size_t pitch = static_cast<size_t>(scales.blocks) * 16;
+  const size_t step = static_cast<size_t>(gridDim.y) * (kMxThreads >> g.log_x);
+  uint8_t* my_stage = stage[ANY ? threadIdx.x >> 5 : 0];
+  const size_t warp_row = (threadIdx.x & ~31u) >> g.log_x, my_row = (threadIdx.x >> g.log_x) - warp_row;
+  for (size_t base = blockIdx.y * static_cast<size_t>(kMxThreads >> g.log_x) + warp_row; base < g.rows; base += kMxUnroll * step) {
+    uint2 w[kMxUnroll];
+    uint32_t s[kMxUnroll];
 #pragma unroll
     for (int j = 0; j < kMxUnroll; ++j) {
-      const int u = base + j * halves;
-      w[j] = 0; s[j] = kScaleOne;
-      if (u >= units) continue;
-      int g;
-      const size_t r = fd_pieces.divmod(u, &g);
-      const int b = g * 4 + (lane16 >> 2);
-      if (b >= scales.blocks) continue;
-      const size_t at = r * code_pitch + g * 64 + lane16 * 4;
-      const size_t sat = scales.tiles ? mx_tile_word(r, g, scales.tiles_k) + (b & 3) : r * static_cast<size_t>(scales.blocks) + b;
-      if (!QC_IN(at + 3, rows * code_pitch) || !QC_IN(sat, scales.extent)) continue;
-      w[j] = __ldg(reinterpret_cast<const uint32_t*>(codes + at));
+      const size_t r = base + j * step + my_row;
+      w[j] = make_uint2(0u, 0u);
+      s[j] = kScaleOne;
+      const size_t at = r * pitch + col / 2;
+      const size_t sat = scales.tiles ? mx_tile_word(r, b >> 2, scales.tiles_k) + (b & 3) : r * static_cast<size_t>(scales.blocks) + b;
+      if (r >= g.rows || b >= scales.blocks || !QC_IN(at + E / 2 - 1, g.rows * pitch) || !QC_IN(sat, scales.extent)) continue;
+      if constexpr (E == 8) w[j].x = __ldg(reinterpret_cast<const uint32_t*>(codes + at));
+      else w[j] = __ldg(reinterpret_cast<const uint2*>(codes + at));
       s[j] = __ldg(scales.bytes + sat);
     }
 #pragma unroll
     for (int j = 0; j < kMxUnroll; ++j) {
-      const int u = base + j * halves;
-      if (u >= units) break;
-      int g;
-      const size_t r = fd_pieces.divmod(u, &g);
-      const int col = g * 128 + lane16 * 8, n = K - col;
-      if (n <= 0 || !QC_IN(r * ld + col + min(n, 8) - 1, (rows - 1) * ld + K)) continue;
-      float v[8];
-      mx_decode_eight(w[j], scale_of(s[j]), v);
-      if (vec_ok && n >= 8) {
-        Eight<T> e;
-        e.pack(v);
-        e.store(y + r * ld + col);
-      } else {
-        store_some(y + r * ld + col, n, v);
-      }
+      const size_t r = base + j * step + my_row;
+      float v[E];
+      mx_decode_eight(w[j].x, scale_of(s[j]), v);
+      if constexpr (E == 16) mx_decode_eight(w[j].y, scale_of(s[j]), v + 8);
+      Piece<T> p;
+      p.pack(v);
+      const int n = r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0;
+      group_store<ANY>(p, y + r * g.ld + first, n, G, lane, g.how, my_stage);
     }
   }
 }

@@ -7,7 +7,7 @@
 // are whole numbers, and a last-bit difference in r would move those that lie next to a border.
 //
 // Bound by HBM: x, residual and h once, the codes once.  A row's values stay in registers from the load to the
-// conversion: W warps a row with V vectors of eight values a thread.
+// conversion: V pieces of 32 bytes a thread, and as many lanes or warps as that makes for the row's length.
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
@@ -15,6 +15,7 @@
 namespace qc {
 
 enum : int { NORM_I8 = 0, NORM_I8_ROWS = 1, NORM_MX = 2 };
+constexpr int kNormMaxWarps = 32;
 
 template <typename T>
 struct NormArgs {
@@ -23,209 +24,288 @@ struct NormArgs {
   const T* gain;
   T* sum;                 // or null; may be x or residual
   size_t ld_x, ld_res, ld_sum, rows;
-  int C, vec_ok, code_vec; // whole vectors of eight values are aligned; eight int8 codes are
+  int C, how, how_gain;   // how: ROWS_* of x, residual and sum together
+  int code_vec;           // a lane's int8 codes are aligned
   double eps;
   float inv;              // NORM_I8: 2^-e
   uint8_t* codes;
   MxScales scales;        // NORM_I8_ROWS: bytes alone
 };
 
-template <int W> constexpr int kNormThreads = W >= 4 ? 32 * W : 128;   // of a block
+// How the threads share out rows: a row is G lanes of a warp (a power of two, at least those of a scale word), or all of the
+// block's warps (G = 32).
+struct NormPlace {
+  size_t row;
+  int G, lane;            // lane within the group
+  int warp, warps;        // warps of the row
+  bool valid;
+};
 
-// Sum over a row's W warps; every thread gets it.
-template <int W>
-__device__ __forceinline__ double row_sum(double v, double* shared) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-  if constexpr (W > 1) {
-    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+// Sum and maximum over a row; all of its threads get them.
+__device__ __forceinline__ double row_sum(double v, double* shared, const NormPlace& at) {
+  for (int d = at.G >> 1; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  if (at.warps > 1) {
+    if (at.lane == 0) shared[at.warp] = v;
     __syncthreads();
-    v = shared[threadIdx.x & (W - 1)];
+    v = at.lane < at.warps ? shared[at.lane] : 0.0;
 #pragma unroll
-    for (int d = W / 2; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
   }
   return v;
 }
-template <int W>
-__device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* shared) {
-  m = __reduce_max_sync(0xffffffffu, m);
-  if constexpr (W > 1) {
-    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
+__device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* shared, const NormPlace& at) {
+  for (int d = at.G >> 1; d > 0; d >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (at.warps > 1) {
+    if (at.lane == 0) shared[at.warp] = m;
     __syncthreads();
-    m = __reduce_max_sync(0xffffffffu, shared[threadIdx.x & (W - 1)]);
+    m = __reduce_max_sync(0xffffffffu, at.lane < at.warps ? shared[at.lane] : 0u);
   }
   return m;
 }
 
-// h of the eight values from `col` on, n of them in the row: loaded, added, rounded, kept.
-template <typename T>
-__device__ __forceinline__ void norm_load(const NormArgs<T>& a, size_t row, int col, float (&h)[8]) {
-  const int n = a.C - col;
-  const T* px = a.x + row * a.ld_x + col;
-  const T* pr = a.residual + row * a.ld_res + col;
-  if (n >= 8 && a.vec_ok && QC_IN(row, a.rows)) {
-    Eight<T> e, f;
-    e.load_written(px);
-    if (a.residual) f.load_written(pr);
-    e.unpack(h);
-    if (a.residual) {
-      float g[8];
-      f.unpack(g);
+// What a lane has loaded of x and the residual, before it is added up.
+template <typename T, bool ANY> struct NormRaw {
+  Piece<T> x, r;
+};
+template <typename T> struct NormRaw<T, true> {
+  T x[Piece<T>::E], r[Piece<T>::E];
+};
+
+// The group's pieces from column `first` on: loaded (all of a thread's loads come before the first use) ...
+template <typename T, bool ANY>
+__device__ __forceinline__ void norm_fetch(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T, ANY>& raw) {
+  constexpr int E = Piece<T>::E;
+  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
+  const T* px = a.x + at.row * a.ld_x + first;
+  const T* pr = a.residual + at.row * a.ld_res + first;
+  if constexpr (ANY) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] += g[i];
-      e.pack(h);                                            // (the rounding to T)
-      e.unpack(h);
-    }
-    if (a.sum) e.store(a.sum + row * a.ld_sum + col);
-  } else if (n > 0 && QC_IN(row, a.rows)) {
-    load_some(px, n, h);
-    if (a.residual) {
-      float g[8];
-      load_some(pr, n, g);
+    for (int i = 0; i < E; ++i) raw.x[i] = i * at.G + at.lane < n ? px[i * at.G + at.lane] : from_float<T>(0.0f);
+    if (a.residual)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = to_float(from_float<T>(h[i] + g[i]));
-    }
-    if (a.sum) store_some(a.sum + row * a.ld_sum + col, n, h);
+      for (int i = 0; i < E; ++i) raw.r[i] = i * at.G + at.lane < n ? pr[i * at.G + at.lane] : from_float<T>(0.0f);
   } else {
-    load_some(px, 0, h);
+    group_load<false>(raw.x, px, n, at.G, at.lane, a.how, nullptr);
+    if (a.residual) group_load<false>(raw.r, pr, n, at.G, at.lane, a.how, nullptr);
+  }
+}
+// ... and h of them: added, rounded, kept.
+template <typename T, bool ANY>
+__device__ __forceinline__ void norm_add(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T, ANY>& raw, Piece<T>& h, uint8_t* stage) {
+  constexpr int E = Piece<T>::E;
+  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
+  if constexpr (ANY) {
+    // (still one value a lane, neighbouring lanes neighbouring values)
+    if (a.residual)
+#pragma unroll
+      for (int i = 0; i < E; ++i) raw.x[i] = from_float<T>(to_float(raw.x[i]) + to_float(raw.r[i]));
+    if (a.sum) {
+      T* ps = a.sum + at.row * a.ld_sum + first;
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (i * at.G + at.lane < n) ps[i * at.G + at.lane] = raw.x[i];
+    }
+    group_arrange(h, raw.x, at.G, at.lane, stage);
+  } else {
+    h = raw.x;
+    if (a.residual) {
+      float v[E], u[E];
+      raw.x.unpack(v);
+      raw.r.unpack(u);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] += u[i];
+      h.pack(v);                                            // (the rounding to T)
+    }
+    if (a.sum) group_store<false>(h, a.sum + at.row * a.ld_sum + first, n, at.G, at.lane, a.how, nullptr);
   }
 }
 
-// y of those values (zeros behind the row's end).
 template <typename T>
-__device__ __forceinline__ void norm_scale(const NormArgs<T>& a, int col, float r, float (&h)[8]) {
-  const int n = a.C - col;
-  float g[8];
-  if (n >= 8 && a.vec_ok) {
-    Eight<T> e;
-    e.load(a.gain + col);
-    e.unpack(g);
-  } else {
-    load_some(a.gain + min(col, a.C), n, g);
-  }
+__device__ __forceinline__ double add_squares(const Piece<T>& h, double sum) {
+  float v[Piece<T>::E];
+  h.unpack(v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) h[i] = (h[i] * r) * g[i];
+  for (int i = 0; i < Piece<T>::E; ++i) sum = fma(static_cast<double>(v[i]), static_cast<double>(v[i]), sum);
+  return sum;
+}
+
+// y of those pieces (zeros behind the row's end).
+template <typename T>
+__device__ __forceinline__ void norm_scale(const NormArgs<T>& a, const NormPlace& at, int first, float r, const Piece<T>& h, float (&y)[Piece<T>::E]) {
+  constexpr int E = Piece<T>::E;
+  Piece<T> g;
+  float u[E];
+  if (a.how_gain != ROWS_ANY) {
+    group_load<false>(g, a.gain + first, a.C - first, at.G, at.lane, a.how_gain, nullptr);
+    g.unpack(u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) u[i] = first + at.lane * E + i < a.C ? to_float(a.gain[first + at.lane * E + i]) : 0.0f;
+  }
+  h.unpack(y);
+#pragma unroll
+  for (int i = 0; i < E; ++i) y[i] = (y[i] * r) * u[i];
 }
 
 template <typename T>
-__device__ __forceinline__ void norm_store_i8(const NormArgs<T>& a, size_t row, int col, const float (&y)[8], float inv) {
-  const int n = min(8, a.C - col);
-  if (n <= 0 || !QC_IN(row, a.rows)) return;
-  const uint2 c = i8_encode_eight(y, inv);
-  uint8_t* p = a.codes + row * a.C + col;
-  if (n == 8 && a.code_vec) *reinterpret_cast<uint2*>(p) = c;
-  else
-    for (int i = 0; i < n; ++i) p[i] = static_cast<uint8_t>((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
+__device__ __forceinline__ void norm_store_i8(const NormArgs<T>& a, const NormPlace& at, int first, const float (&y)[Piece<T>::E], float inv, uint8_t* stage) {
+  constexpr int E = Piece<T>::E;
+  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
+  uint32_t c[E / 4];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) c[i] = i8_encode_four(y + 4 * i, inv);
+  uint8_t* p = a.codes + at.row * a.C + first;
+  if (a.code_vec) {                                         // (C is then a multiple of E, too)
+    if (at.lane * E >= n) return;
+    if constexpr (E == 8) *reinterpret_cast<uint2*>(p + at.lane * E) = make_uint2(c[0], c[1]);
+    else *reinterpret_cast<uint4*>(p + at.lane * E) = make_uint4(c[0], c[1], c[2], c[3]);
+  } else {
+    // neighbouring lanes write neighbouring bytes
+    uint8_t* mine = stage + ((threadIdx.x & 31) - at.lane) * E;
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) reinterpret_cast<uint32_t*>(mine)[at.lane * (E / 4) + i] = c[i];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (i * at.G + at.lane < n) p[i * at.G + at.lane] = mine[i * at.G + at.lane];
+    __syncwarp();
+  }
 }
 
-// Whole warps: four lanes a block, sixteen a scale word.
 template <typename T>
-__device__ __forceinline__ void norm_store_mx(const NormArgs<T>& a, size_t row, int col, float (&y)[8]) {
-  const uint32_t s = mx_scale_byte(finite_top<4>(y), 0x3FFFFFu);
-  const uint32_t word = gather_scale_word(s);
+__device__ __forceinline__ void norm_store_mx(const NormArgs<T>& a, const NormPlace& at, int first, float (&y)[Piece<T>::E]) {
+  constexpr int E = Piece<T>::E, kBlockLanes = kMxBlock / E;
+  const int col = first + at.lane * E;
+  const uint32_t s = mx_scale_byte(finite_top<kBlockLanes>(y, top_bits(y)), kCoverRoundUp);
+  const uint32_t word = gather_scale_word<kBlockLanes>(s);
   const int padded = a.scales.blocks * kMxBlock;
-  if (!QC_IN(row, a.rows)) return;
-  if (col < padded) *reinterpret_cast<uint32_t*>(a.codes + row * static_cast<size_t>(padded / 2) + col / 2) = mx_encode_eight(y, inverse_scale(s));
-  if ((col & 127) == 0 && col < padded) store_scale_word(a.scales, row, col >> 7, word);
+  if (!at.valid || !QC_IN(at.row, a.rows) || col >= padded) return;
+  mx_store_codes(a.codes + at.row * static_cast<size_t>(padded / 2) + col / 2, y, inverse_scale(s));
+  if ((col & 127) == 0) store_scale_word(a.scales, at.row, col >> 7, word);
 }
 
-// Scale words of the rows that fill up the last tile of 128: shared out among the tile's real rows.
+// Scale words of the rows that fill up the last tile of 128, by `blocks` blocks of which this is number `block`.
 template <typename T>
-__device__ __forceinline__ void norm_pad_rows(const NormArgs<T>& a, size_t row, int tid, int threads) {
+__device__ __forceinline__ void norm_pad_rows(const NormArgs<T>& a, int block, int blocks) {
   const size_t tile0 = (a.rows - 1) & ~static_cast<size_t>(kMxTileRows - 1);
-  if (!a.scales.tiles || row < tile0) return;
-  for (size_t p = a.rows + (row - tile0); p < tile0 + kMxTileRows; p += a.rows - tile0)
-    for (int t = tid; t < a.scales.tiles_k; t += threads) store_scale_word(a.scales, p, t, 0x01010101u * kScaleOne);
+  const int real = static_cast<int>(a.rows - tile0), threads = blockDim.x * blockDim.y;
+  // word i of the last row of tiles is word i % 128 of tile i / 128, and that is row i % 128 / 4 + 32 (i % 4)
+  const int words = a.scales.tiles_k * kMxTileRows;
+  for (int i = block * threads + threadIdx.y * blockDim.x + threadIdx.x; i < words; i += blocks * threads) {
+    const int r = (i & 127) >> 2 | (i & 3) << 5;
+    if (r >= real) store_scale_word(a.scales, tile0 + r, i >> 7, 0x01010101u * kScaleOne);
+  }
 }
 
 __device__ __forceinline__ float norm_factor(double sum, int C, double eps) {
   return static_cast<float>(1.0 / sqrt(sum / C + eps));
 }
 
-template <typename T, int OUT, int W, int V>
-__global__ void __launch_bounds__(kNormThreads<W>)
-rmsnorm_kernel(const NormArgs<T> a) {
-  __shared__ double sums[W];
-  __shared__ uint32_t tops[W];
+// Blocks behind those of the rows (row_blocks of them) write the padding scale words.
+template <typename T, int OUT, int V, bool ANY>
+__global__ void __launch_bounds__(V == 1 ? 1024 : 512)
+rmsnorm_kernel(const NormArgs<T> a, int G, unsigned int row_blocks) {
+  constexpr int E = Piece<T>::E;
+  __shared__ double sums[kNormMaxWarps];
+  __shared__ uint32_t tops[kNormMaxWarps];
+  extern __shared__ uint8_t stages[];                       // kWarpStage a warp; none where everything is aligned
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  constexpr int kRows = kNormThreads<W> / (32 * W);       // rows of a block
-  const int tid = W == 1 ? threadIdx.x & 31 : threadIdx.x;  // thread of the row
-  const size_t row = static_cast<size_t>(blockIdx.x) * kRows + (W == 1 ? threadIdx.x >> 5 : 0);
-  if (row >= a.rows) return;                                // (a whole warp, and only where a row is one warp)
-  float h[V][8];
+  if constexpr (OUT == NORM_MX) {
+    if (blockIdx.x >= row_blocks) { norm_pad_rows(a, blockIdx.x - row_blocks, gridDim.x - row_blocks); return; }
+  }
+  // the rows of a warp (blockDim.y warps a block), or one row a block
+  NormPlace at;
+  at.G = G; at.lane = threadIdx.x & (G - 1);
+  at.warp = threadIdx.x >> 5; at.warps = blockDim.x >> 5;
+  at.row = (static_cast<size_t>(blockIdx.x) * blockDim.y + threadIdx.y) * (32 / G) + (at.warps > 1 ? 0 : threadIdx.x / G);
+  at.valid = at.row < a.rows;
+  uint8_t* stage = stages + (at.warp + threadIdx.y) * kWarpStage;
+  Piece<T> h[V];
+  {
+    NormRaw<T, ANY> raw[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) norm_fetch(a, at, (v * at.warps + at.warp) * 32 * E, raw[v]);
+#pragma unroll
+    for (int v = 0; v < V; ++v) norm_add(a, at, (v * at.warps + at.warp) * 32 * E, raw[v], h[v], stage);
+  }
   double sum = 0.0;
 #pragma unroll
-  for (int v = 0; v < V; ++v) norm_load(a, row, (v * W * 32 + tid) * 8, h[v]);
+  for (int v = 0; v < V; ++v) sum = add_squares(h[v], sum);
+  const float r = norm_factor(row_sum(sum, sums, at), a.C, a.eps);
+  if constexpr (OUT == NORM_I8_ROWS) {
+    float y[V][E];
+    uint32_t m = 0;
 #pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fma(static_cast<double>(h[v][i]), static_cast<double>(h[v][i]), sum);
-  const float r = norm_factor(row_sum<W>(sum, sums), a.C, a.eps);
-#pragma unroll
-  for (int v = 0; v < V; ++v) norm_scale(a, (v * W * 32 + tid) * 8, r, h[v]);
-  if constexpr (OUT == NORM_MX) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) norm_store_mx(a, row, (v * W * 32 + tid) * 8, h[v]);
-    norm_pad_rows(a, row, tid, 32 * W);
-  } else {
-    float inv = a.inv;
-    if constexpr (OUT == NORM_I8_ROWS) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) m = max(m, finite_top<1>(h[v]));
-      const uint32_t s = i8_scale_byte(row_max<W>(m, tops));
-      inv = inverse_scale(s);
-      if (tid == 0) a.scales.bytes[row] = static_cast<uint8_t>(s);
+    for (int v = 0; v < V; ++v) {
+      norm_scale(a, at, (v * at.warps + at.warp) * 32 * E, r, h[v], y[v]);
+      m = max(m, finite_top<1>(y[v], top_bits(y[v])));
     }
+    const uint32_t s = i8_scale_byte(row_max(m, tops, at));
+    if (at.lane == 0 && at.warp == 0 && at.valid) a.scales.bytes[at.row] = static_cast<uint8_t>(s);
 #pragma unroll
-    for (int v = 0; v < V; ++v) norm_store_i8(a, row, (v * W * 32 + tid) * 8, h[v], inv);
+    for (int v = 0; v < V; ++v) norm_store_i8(a, at, (v * at.warps + at.warp) * 32 * E, y[v], inverse_scale(s), stage);
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int first = (v * at.warps + at.warp) * 32 * E;
+      float y[E];
+      norm_scale(a, at, first, r, h[v], y);
+      if constexpr (OUT == NORM_MX) norm_store_mx(a, at, first, y);
+      else norm_store_i8(a, at, first, y, a.inv, stage);
+    }
   }
 }
 
-// Rows longer than the registers of a block hold: one block a row, h read again (from where it was kept, else made again)
-// for each further step.
-constexpr int kNormLongWarps = 32;
-template <typename T, int OUT>
-__global__ void __launch_bounds__(32 * kNormLongWarps)
-rmsnorm_long_kernel(const NormArgs<T> a) {
-  __shared__ double sums[kNormLongWarps];
-  __shared__ uint32_t tops[kNormLongWarps];
+// Rows longer than the registers of a block hold: one block a row, h read again (from where it was kept, by the thread that
+// kept it, else made again) for each further step.
+template <typename T, int OUT, bool ANY>
+__global__ void __launch_bounds__(32 * kNormMaxWarps)
+rmsnorm_long_kernel(const NormArgs<T> a, unsigned int row_blocks) {
+  constexpr int E = Piece<T>::E, kStep = kNormMaxWarps * 32 * E;
+  __shared__ double sums[kNormMaxWarps];
+  __shared__ uint32_t tops[kNormMaxWarps];
+  extern __shared__ uint8_t stages[];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const size_t row = blockIdx.x;
-  constexpr int kStep = kNormLongWarps * 32 * 8;
-  const int first = threadIdx.x * 8;
+  if constexpr (OUT == NORM_MX) {
+    if (blockIdx.x >= row_blocks) { norm_pad_rows(a, blockIdx.x - row_blocks, gridDim.x - row_blocks); return; }
+  }
+  const NormPlace at = {blockIdx.x, 32, static_cast<int>(threadIdx.x & 31), static_cast<int>(threadIdx.x >> 5), kNormMaxWarps, true};
+  uint8_t* stage = stages + at.warp * kWarpStage;
   NormArgs<T> again = a;
   if (a.sum) { again.x = a.sum; again.ld_x = a.ld_sum; again.residual = nullptr; }
   again.sum = nullptr;
-  float h[8];
+  Piece<T> h;
+  NormRaw<T, ANY> raw;
+  float y[E];
   double sum = 0.0;
-  for (int col = first; col - first < a.C; col += kStep) {
-    norm_load(a, row, col, h);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fma(static_cast<double>(h[i]), static_cast<double>(h[i]), sum);
+  for (int first = at.warp * 32 * E; first < a.C; first += kStep) {
+    norm_fetch(a, at, first, raw);
+    norm_add(a, at, first, raw, h, stage);
+    sum = add_squares(h, sum);
   }
-  const float r = norm_factor(row_sum<kNormLongWarps>(sum, sums), a.C, a.eps);
+  const float r = norm_factor(row_sum(sum, sums, at), a.C, a.eps);
   float inv = a.inv;
   if constexpr (OUT == NORM_I8_ROWS) {
     uint32_t m = 0;
-    for (int col = first; col - first < a.C; col += kStep) {
-      norm_load(again, row, col, h);
-      norm_scale(a, col, r, h);
-      m = max(m, finite_top<1>(h));
+    for (int first = at.warp * 32 * E; first < a.C; first += kStep) {
+      norm_fetch(again, at, first, raw);
+      norm_add(again, at, first, raw, h, stage);
+      norm_scale(a, at, first, r, h, y);
+      m = max(m, finite_top<1>(y, top_bits(y)));
     }
-    const uint32_t s = i8_scale_byte(row_max<kNormLongWarps>(m, tops));
+    const uint32_t s = i8_scale_byte(row_max(m, tops, at));
     inv = inverse_scale(s);
-    if (threadIdx.x == 0) a.scales.bytes[row] = static_cast<uint8_t>(s);
+    if (threadIdx.x == 0) a.scales.bytes[at.row] = static_cast<uint8_t>(s);
   }
-  for (int col = first; col - first < a.C; col += kStep) {
-    norm_load(again, row, col, h);
-    norm_scale(a, col, r, h);
-    if constexpr (OUT == NORM_MX) norm_store_mx(a, row, col, h);
-    else norm_store_i8(a, row, col, h, inv);
+  for (int first = at.warp * 32 * E; first < a.C; first += kStep) {
+    norm_fetch(again, at, first, raw);
+    norm_add(again, at, first, raw, h, stage);
+    norm_scale(a, at, first, r, h, y);
+    if constexpr (OUT == NORM_MX) norm_store_mx(a, at, first, y);
+    else norm_store_i8(a, at, first, y, inv, stage);
   }
-  if constexpr (OUT == NORM_MX) norm_pad_rows(a, row, threadIdx.x, 32 * kNormLongWarps);
 }
 
 }  // namespace qc

@@ -78,8 +78,28 @@ int check_values(const void* p, int type, long long ld, int width, const char* w
   if (!aligned(p, type_size(type))) return fail(QCONV_ERR_ALIGNMENT, "%s must be aligned to its type", what);
   return QCONV_OK;
 }
-// Rows of eight-value vectors at 16-byte boundaries.
-int vectors_ok(const void* p, int type, long long ld) { return aligned(p, 16) && ld * type_size(type) % 16 == 0; }
+// How rows from p on, `ld` elements apart, may be reached (ROWS_*).
+int reach(const void* p, int type, long long ld) {
+  const long long bytes = ld * static_cast<long long>(type_size(type));
+  return aligned(p, 32) && bytes % 32 == 0 ? qc::ROWS_32 : aligned(p, 16) && bytes % 16 == 0 ? qc::ROWS_16 : qc::ROWS_ANY;
+}
+
+// The blocks of a conversion over `rows_out` rows: enough lanes along the row, and rows until the device is full.
+qc::MxGrid mx_grid(long long rows, long long rows_out, int K, long long ld, int type, const void* values, dim3* grid) {
+  const int E = 32 / static_cast<int>(type_size(type));
+  const int lanes = qc::mx_blocks(K) * (qc::kMxBlock / E);
+  qc::MxGrid g = {};
+  g.lanes_x = 128 / E;                                     // of a scale word
+  g.log_x = E == 8 ? 4 : 3;
+  while (g.lanes_x < qc::kMxThreads && g.lanes_x < lanes) { g.lanes_x *= 2; ++g.log_x; }
+  g.rows = static_cast<size_t>(rows); g.rows_out = static_cast<size_t>(rows_out); g.K = K; g.ld = static_cast<size_t>(ld);
+  g.how = reach(values, type, ld);
+  const long long per_block = qc::kMxThreads / g.lanes_x;
+  grid->x = static_cast<unsigned int>((lanes + g.lanes_x - 1) / g.lanes_x);
+  const long long most = std::max(1ll, 148ll * 16 / grid->x);
+  grid->y = static_cast<unsigned int>(std::min({(rows_out + per_block - 1) / per_block, most, 65535ll}));
+  return g;
+}
 
 }  // namespace
 
@@ -118,15 +138,13 @@ int qmx_quantize(const void* d_x, int type, long long rows, int K, long long ld,
   if (!rc) rc = check_values(d_x, type, ld, K, "x");
   if (!rc) rc = check_code_alignment(d_codes, d_scales, layout);
   if (rc) return rc;
-  const int pieces = (K + 127) / 128;
-  const int units = static_cast<int>((layout == QMX_TILES ? (rows + 127) / 128 * 128 : rows) * pieces);
-  const int grid = qc::grid_for((units + 15ll) / 16, 1, 148 * 8);
+  dim3 grid;
+  const qc::MxGrid g = mx_grid(rows, layout == QMX_TILES ? (rows + 127) / 128 * 128 : rows, K, ld, type, d_x, &grid);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    CUDA_TRY(launch_chained(qc::mx_quantize_kernel<T>, dim3(grid), dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream),
-                            static_cast<const T*>(d_x), static_cast<size_t>(ld), static_cast<size_t>(rows), K, d_codes,
-                            make_scales(d_scales, rows, K, layout), rule == QMX_COVER ? 0x3FFFFFu : 0u, units, make_fastdiv(pieces),
-                            vectors_ok(d_x, type, ld)));
+    const auto kernel = g.how == qc::ROWS_ANY ? qc::mx_quantize_kernel<T, true> : qc::mx_quantize_kernel<T, false>;
+    CUDA_TRY(launch_chained(kernel, grid, dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream), static_cast<const T*>(d_x), g, d_codes,
+                            make_scales(d_scales, rows, K, layout), rule == QMX_COVER ? qc::kCoverRoundUp : 0u));
     return static_cast<int>(QCONV_OK);
   });
 }
@@ -139,14 +157,13 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
   if (!rc) rc = check_values(d_y, type, ld, K, "y");
   if (!rc) rc = check_code_alignment(d_codes, d_scales, layout);
   if (rc) return rc;
-  const int pieces = (K + 127) / 128;
-  const int units = static_cast<int>(rows * pieces);
-  const int grid = qc::grid_for((units + 15ll) / 16, 1, 148 * 8);
+  dim3 grid;
+  const qc::MxGrid g = mx_grid(rows, rows, K, ld, type, d_y, &grid);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    CUDA_TRY(launch_chained(qc::mx_dequantize_kernel<T>, dim3(grid), dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream),
-                            d_codes, make_scales(const_cast<uint8_t*>(d_scales), rows, K, layout), static_cast<size_t>(rows), K,
-                            static_cast<T*>(d_y), static_cast<size_t>(ld), units, make_fastdiv(pieces), vectors_ok(d_y, type, ld)));
+    const auto kernel = g.how == qc::ROWS_ANY ? qc::mx_dequantize_kernel<T, true> : qc::mx_dequantize_kernel<T, false>;
+    CUDA_TRY(launch_chained(kernel, grid, dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream), d_codes,
+                            make_scales(const_cast<uint8_t*>(d_scales), rows, K, layout), g, static_cast<T*>(d_y)));
     return static_cast<int>(QCONV_OK);
   });
 }
@@ -380,25 +397,47 @@ int qmx_linear_destroy(qmx_linear* h) {
 
 namespace {
 
-template <typename T, int OUT, int W, int V>
-int launch_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
-  constexpr int threads = qc::kNormThreads<W>, rows = threads / (32 * W);
-  CUDA_TRY(launch_chained(qc::rmsnorm_kernel<T, OUT, W, V>, dim3(static_cast<unsigned int>((a.rows + rows - 1) / rows)), dim3(threads), 0, st, a));
-  return QCONV_OK;
+// Blocks that write the scale bytes of rows which only fill up the last tile.
+template <int OUT, typename T>
+unsigned int pad_blocks(const qc::NormArgs<T>& a) {
+  if (OUT != qc::NORM_MX || !a.scales.tiles || a.rows % qc::kMxTileRows == 0) return 0;
+  return static_cast<unsigned int>(std::min(16, (a.scales.tiles_k * qc::kMxTileRows + 1023) / 1024));
 }
 
 template <typename T, int OUT>
+size_t norm_stages(const qc::NormArgs<T>& a, int warps) {
+  return a.how == qc::ROWS_ANY || (OUT != qc::NORM_MX && !a.code_vec) ? static_cast<size_t>(warps) * qc::kWarpStage : 0;
+}
+
+// G lanes of a warp a row (four warps a block), or `warps` warps.
+template <typename T, int OUT, int V>
+int launch_norm(const qc::NormArgs<T>& a, int G, int warps, cudaStream_t st) {
+  const unsigned int y = warps == 1 ? 4 : 1;
+  const size_t per_block = static_cast<size_t>(y) * (32 / G);
+  const unsigned int blocks = static_cast<unsigned int>((a.rows + per_block - 1) / per_block);
+  const auto kernel = a.how == qc::ROWS_ANY ? qc::rmsnorm_kernel<T, OUT, V, true> : qc::rmsnorm_kernel<T, OUT, V, false>;
+  CUDA_TRY(launch_chained(kernel, dim3(blocks + pad_blocks<OUT>(a)), dim3(32 * warps, y), norm_stages<T, OUT>(a, warps * static_cast<int>(y)), st, a, G, blocks));
+  return QCONV_OK;
+}
+
+// A row's values in registers: pieces of 32 bytes, one a lane for few rows (the more warps, the shorter the chain of a
+// thread), two or four for many.
+template <typename T, int OUT>
 int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
-  if (a.C <= 256) return launch_norm<T, OUT, 1, 1>(a, st);
-  if (a.C <= 1024) return a.rows >= 1024 ? launch_norm<T, OUT, 1, 4>(a, st) : launch_norm<T, OUT, 4, 1>(a, st);
-  if (a.rows < 512) {
-    if (a.C <= 4096) return launch_norm<T, OUT, 16, 1>(a, st);
-    if (a.C <= 8192) return launch_norm<T, OUT, 32, 1>(a, st);
+  constexpr int E = qc::Piece<T>::E;
+  const int lanes = (OUT == qc::NORM_MX ? qc::mx_blocks(a.C) * qc::kMxBlock : a.C + E - 1) / E;
+  const auto warps = [&](int v) { return (lanes + 32 * v - 1) / (32 * v); };
+  if (lanes <= 32) {
+    int G = 128 / E;                                        // lanes of a scale word
+    while (G < lanes) G *= 2;
+    return launch_norm<T, OUT, 1>(a, G, 1, st);
   }
-  if (a.C <= 4096) return launch_norm<T, OUT, 4, 4>(a, st);
-  if (a.C <= 8192) return launch_norm<T, OUT, 8, 4>(a, st);
-  if (a.C <= 16384) return launch_norm<T, OUT, 16, 4>(a, st);
-  CUDA_TRY(launch_chained(qc::rmsnorm_long_kernel<T, OUT>, dim3(static_cast<unsigned int>(a.rows)), dim3(32 * qc::kNormLongWarps), 0, st, a));
+  if (lanes <= 1024 && a.rows < 512) return launch_norm<T, OUT, 1>(a, 32, warps(1), st);
+  if (lanes <= 1024) return launch_norm<T, OUT, 2>(a, 32, warps(2), st);
+  if (lanes <= 2048) return launch_norm<T, OUT, 4>(a, 32, warps(4), st);
+  const auto kernel = a.how == qc::ROWS_ANY ? qc::rmsnorm_long_kernel<T, OUT, true> : qc::rmsnorm_long_kernel<T, OUT, false>;
+  const unsigned int blocks = static_cast<unsigned int>(a.rows);
+  CUDA_TRY(launch_chained(kernel, dim3(blocks + pad_blocks<OUT>(a)), dim3(32 * qc::kNormMaxWarps), norm_stages<T, OUT>(a, qc::kNormMaxWarps), st, a, blocks));
   return QCONV_OK;
 }
 
@@ -436,9 +475,11 @@ int qrmsnorm(const qrmsnorm_args* args, void* cuda_stream) {
     a.sum = static_cast<T*>(g.d_sum);
     a.ld_x = g.ld_x; a.ld_res = g.d_residual ? g.ld_residual : 0; a.ld_sum = g.d_sum ? g.ld_sum : 0;
     a.rows = g.rows; a.C = g.C; a.eps = g.eps;
-    a.vec_ok = vectors_ok(g.d_x, g.type, g.ld_x) && aligned(g.d_gain, 16) && (!g.d_residual || vectors_ok(g.d_residual, g.type, g.ld_residual)) &&
-               (!g.d_sum || vectors_ok(g.d_sum, g.type, g.ld_sum));
-    a.code_vec = aligned(g.d_codes, 8) && g.C % 8 == 0;
+    a.how = reach(g.d_x, g.type, g.ld_x);
+    a.how_gain = reach(g.d_gain, g.type, 0);
+    if (g.d_residual) a.how = std::min(a.how, reach(g.d_residual, g.type, g.ld_residual));
+    if (g.d_sum) a.how = std::min(a.how, reach(g.d_sum, g.type, g.ld_sum));
+    a.code_vec = aligned(g.d_codes, qc::Piece<T>::E) && g.C % qc::Piece<T>::E == 0;
     a.inv = std::ldexp(1.0f, -g.e);
     a.codes = g.d_codes;
     if (g.out == QNORM_MX) a.scales = make_scales(g.d_scales, g.rows, g.C, g.layout);
@@ -472,8 +513,9 @@ int cache_args(const qcache_desc* c, const qcache_values* keys, const qcache_val
   a->fd_heads = make_fastdiv(c->heads);
   a->code_pitch = c->format == QCACHE_I8 ? c->D : a->blocks * 16;
   a->scale_pitch = c->format == QCACHE_I8 ? 1 : a->blocks;
-  a->vec_ok = 1;
-  a->code_vec = c->D % 8 == 0;
+  const int per_lane = 32 / static_cast<int>(type_size(type));
+  a->how = qc::ROWS_32;
+  a->code_vec = c->D % per_lane == 0;
   const qcache_values* in[2] = {keys, values};
   uint8_t* codes[2] = {c->d_k_codes, c->d_v_codes};
   uint8_t* scales[2] = {c->d_k_scales, c->d_v_scales};
@@ -485,26 +527,27 @@ int cache_args(const qcache_desc* c, const qcache_values* keys, const qcache_val
     if (!aligned(v.d_values, type_size(type))) return fail(QCONV_ERR_ALIGNMENT, "values must be aligned to their type");
     if (c->format == QCACHE_MX && !aligned(codes[i], 16)) return fail(QCONV_ERR_ALIGNMENT, "codes must be 16-byte aligned");
     a->side[i] = {codes[i], scales[i], v.d_values, v.token_stride, v.head_stride};
-    a->vec_ok &= vectors_ok(v.d_values, type, v.token_stride) && v.head_stride * type_size(type) % 16 == 0;
-    a->code_vec &= aligned(codes[i], 8);
+    a->how = std::min({a->how, reach(v.d_values, type, v.token_stride), reach(v.d_values, type, v.head_stride)});
+    a->code_vec &= aligned(codes[i], per_lane);
   }
   return QCONV_OK;
 }
 
 template <typename T, int FMT, int LANES, int V>
 int launch_cache(const qc::CacheArgs& a, bool write, cudaStream_t st) {
-  constexpr int per_block = qc::kCacheThreads / LANES;
-  if (write)
-    CUDA_TRY(launch_chained(qc::cache_write_kernel<T, FMT, LANES, V>, dim3(qc::grid_for(a.items, per_block, 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));
-  else
-    CUDA_TRY(launch_chained(qc::cache_read_kernel<T, FMT, LANES, V>, dim3(qc::grid_for(a.items, per_block, 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));
+  const bool any = a.how == qc::ROWS_ANY;
+  const auto kernel = write ? (any ? qc::cache_write_kernel<T, FMT, LANES, V, true> : qc::cache_write_kernel<T, FMT, LANES, V, false>)
+                            : (any ? qc::cache_read_kernel<T, FMT, LANES, V, true> : qc::cache_read_kernel<T, FMT, LANES, V, false>);
+  CUDA_TRY(launch_chained(kernel, dim3(qc::grid_for(a.items, qc::kCacheThreads / LANES, 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));
   return QCONV_OK;
 }
 template <typename T, int FMT>
 int run_cache(const qc::CacheArgs& a, bool write, cudaStream_t st) {
-  if (a.D <= 64) return launch_cache<T, FMT, 8, 1>(a, write, st);
-  if (a.D <= 128) return launch_cache<T, FMT, 16, 1>(a, write, st);
-  if (a.D <= 256) return launch_cache<T, FMT, 32, 1>(a, write, st);
+  const int lanes = (FMT == qc::CACHE_MX ? a.blocks * qc::kMxBlock : a.D) / qc::Piece<T>::E + (FMT == qc::CACHE_I8 && a.D % qc::Piece<T>::E != 0);
+  if (lanes <= 4) return launch_cache<T, FMT, 4, 1>(a, write, st);
+  if (lanes <= 8) return launch_cache<T, FMT, 8, 1>(a, write, st);
+  if (lanes <= 16) return launch_cache<T, FMT, 16, 1>(a, write, st);
+  if (lanes <= 32) return launch_cache<T, FMT, 32, 1>(a, write, st);
   return launch_cache<T, FMT, 32, 4>(a, write, st);
 }
 int run_cache(const qcache_desc* c, const qcache_values* keys, const qcache_values* values, int type, const int64_t* d_slots, long long rows,

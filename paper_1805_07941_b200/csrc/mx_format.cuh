@@ -58,72 +58,166 @@ __device__ __forceinline__ float2 unpack_two(uint32_t w, __half) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// Eight consecutive values of a row, as they lie in memory (16 or 32 bytes).
-template <typename T> struct Eight {
-  uint4 w[sizeof(T) / 2];
-  __device__ __forceinline__ void load(const T* p) {
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// How a row of values may be reached.
+enum : int { ROWS_ANY = 0, ROWS_16 = 1, ROWS_32 = 2 };     // one value at a time; in 16-byte pieces; in 32-byte pieces
+
+// What a lane holds of a row: 32 bytes, E consecutive values (8 float32, 16 of a 16-bit type).
+template <typename T> struct Piece {
+  static constexpr int E = 32 / static_cast<int>(sizeof(T));
+  uint32_t w[8];
+
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < 8; ++i) w[i] = 0u;
   }
-  // The same through the ordinary path, for memory that this kernel also writes.
-  __device__ __forceinline__ void load_written(const T* p) {
-#pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
-  }
-  __device__ __forceinline__ void unpack(float (&v)[8]) const {
-    if constexpr (sizeof(T) == 4) {
-      v[0] = __uint_as_float(w[0].x); v[1] = __uint_as_float(w[0].y); v[2] = __uint_as_float(w[0].z); v[3] = __uint_as_float(w[0].w);
-      v[4] = __uint_as_float(w[1].x); v[5] = __uint_as_float(w[1].y); v[6] = __uint_as_float(w[1].z); v[7] = __uint_as_float(w[1].w);
+  // Whole pieces.  (Ordinary loads, not the read-only path: the memory may be written by this kernel, too.)
+  __device__ __forceinline__ void load(const T* p, int how) {
+    if (how == ROWS_32) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
     } else {
-      const uint32_t q[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+      const uint4 a = *reinterpret_cast<const uint4*>(p), b = *(reinterpret_cast<const uint4*>(p) + 1);
+      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int how) const {
+    if (how == ROWS_32) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                   ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    } else {
+      reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  }
+  __device__ __forceinline__ void unpack(float (&v)[E]) const {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack_two(q[i], T());
+      for (int i = 0; i < E; ++i) v[i] = __uint_as_float(w[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 f = unpack_two(w[i], T());
         v[2 * i] = f.x; v[2 * i + 1] = f.y;
       }
     }
   }
-  __device__ __forceinline__ void pack(const float (&v)[8]) {
+  __device__ __forceinline__ void pack(const float (&v)[E]) {
     if constexpr (sizeof(T) == 4) {
-      w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-      w[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+#pragma unroll
+      for (int i = 0; i < E; ++i) w[i] = __float_as_uint(v[i]);
     } else {
-      w[0] = make_uint4(pack_two(v[0], v[1], T()), pack_two(v[2], v[3], T()), pack_two(v[4], v[5], T()), pack_two(v[6], v[7], T()));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = pack_two(v[2 * i], v[2 * i + 1], T());
     }
   }
-  __device__ __forceinline__ void store(T* p) const {
+  // Bits, as float32's, of the largest magnitude (magnitudes order like their bit patterns, NaN above infinity): for 16-bit
+  // types two at a time.
+  __device__ __forceinline__ uint32_t top() const {
+    if constexpr (sizeof(T) == 4) {
+      uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = w[i];
+      for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+      return m;
+    } else {
+      uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+      for (int i = 1; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+      m = max(m & 0xFFFFu, m >> 16);
+      if constexpr (sizeof(T) == 2 && static_cast<bool>(__is_same(T, __half)))
+        return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(m))));
+      else
+        return m << 16;
+    }
   }
 };
 
-// The first `n` of eight values at p one by one, zeros behind them.
+// Bytes of shared memory a warp needs for rows that are reached one value at a time.
+constexpr int kWarpStage = 1024;
+
+// Lane l of a group of G holds values l, l + G, l + 2 G, ... and gets E consecutive ones, through its warp's shared memory.
 template <typename T>
-__device__ __forceinline__ void load_some(const T* p, int n, float (&v)[8]) {
+__device__ __forceinline__ void group_arrange(Piece<T>& x, const T (&v)[Piece<T>::E], int G, int lane, uint8_t* stage) {
+  constexpr int E = Piece<T>::E;
+  T* mine = reinterpret_cast<T*>(stage) + ((threadIdx.x & 31) - lane) * E;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < n ? to_float(p[i]) : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void store_some(T* p, int n, const float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < n) p[i] = from_float<T>(v[i]);
+  for (int i = 0; i < E; ++i) mine[i * G + lane] = v[i];
+  __syncwarp();
+  const uint4* q = reinterpret_cast<const uint4*>(mine + lane * E);
+  const uint4 a = q[0], b = q[1];
+  x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w; x.w[4] = b.x; x.w[5] = b.y; x.w[6] = b.z; x.w[7] = b.w;
+  __syncwarp();
 }
 
-constexpr uint32_t kInfBits = 0x7F800000u;
+// Loads the pieces of a group of G lanes (a power of two up to 32): G * E consecutive values from p on, of which the first
+// n exist (zeros behind them; n may be negative).  Where 16-byte accesses are not aligned the group reads one value a
+// lane, neighbouring lanes neighbouring values, and passes them through its warp's shared memory.  Whole warps.  ANY: how is
+// ROWS_ANY (an instantiation of its own, so that the aligned one is lean).
+template <bool ANY, typename T>
+__device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G, int lane, int how, uint8_t* stage) {
+  constexpr int E = Piece<T>::E;
+  if constexpr (!ANY) {
+    const int left = n - lane * E;
+    if (left >= E) {
+      x.load(p + lane * E, how);
+    } else {
+      x.clear();
+      if (left > 0) {
+        float v[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = i < left ? to_float(p[lane * E + i]) : 0.0f;
+        x.pack(v);
+      }
+    }
+  } else {
+    T v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = i * G + lane < n ? p[i * G + lane] : from_float<T>(0.0f);
+    group_arrange(x, v, G, lane, stage);
+  }
+}
+// The same way back: the first n values.
+template <bool ANY, typename T>
+__device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int G, int lane, int how, uint8_t* stage) {
+  constexpr int E = Piece<T>::E;
+  if constexpr (!ANY) {
+    const int left = n - lane * E;
+    if (left >= E) {
+      x.store(p + lane * E, how);
+    } else if (left > 0) {
+      float v[E];
+      x.unpack(v);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (i < left) p[lane * E + i] = from_float<T>(v[i]);
+    }
+  } else {
+    T* mine = reinterpret_cast<T*>(stage) + ((threadIdx.x & 31) - lane) * E;
+    uint4* q = reinterpret_cast<uint4*>(mine + lane * E);
+    q[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+    q[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (i * G + lane < n) p[i * G + lane] = mine[i * G + lane];
+    __syncwarp();
+  }
+}
 
-// Bits of the largest |v| (magnitudes order like their bit patterns, NaN above infinity).
-__device__ __forceinline__ uint32_t top_bits(const float (&v)[8]) {
+// Bits of the largest |v| over a lane's values; over the finite ones alone, with NaN made 0 in v (infinities stay: they saturate).
+template <int E>
+__device__ __forceinline__ uint32_t top_bits(const float (&v)[E]) {
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  for (int i = 0; i < E; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
   return m;
 }
-// The same over the finite values alone; NaN becomes 0 in v, infinities stay (they saturate).
-__device__ __forceinline__ uint32_t top_bits_finite(float (&v)[8]) {
+template <int E>
+__device__ __forceinline__ uint32_t top_bits_finite(float (&v)[E]) {
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < E; ++i) {
     const uint32_t a = __float_as_uint(v[i]) & 0x7FFFFFFFu;
     if (a > kInfBits) v[i] = 0.0f;
     else if (a < kInfBits) m = max(m, a);
@@ -136,10 +230,10 @@ __device__ __forceinline__ uint32_t max_over(uint32_t m) {
   for (int d = 1; d < LANES; d *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
   return m;
 }
-// Largest finite magnitude of the 8 LANES values that LANES neighbouring lanes hold; NaN becomes 0 in v.  Whole warps only.
-template <int LANES>
-__device__ __forceinline__ uint32_t finite_top(float (&v)[8]) {
-  uint32_t m = top_bits(v);
+// Largest finite magnitude of the values that LANES neighbouring lanes hold; NaN becomes 0 in v.  m: top_bits of v, if that is
+// known already.  Whole warps only.
+template <int LANES, int E>
+__device__ __forceinline__ uint32_t finite_top(float (&v)[E], uint32_t m) {
   if (__any_sync(0xffffffffu, m >= kInfBits)) m = top_bits_finite(v);
   return max_over<LANES>(m);
 }
@@ -147,6 +241,7 @@ __device__ __forceinline__ uint32_t finite_top(float (&v)[8]) {
 // Scale byte of a block of 4-bit values whose largest finite magnitude has the bits m (0: the block is zero, scale 1).
 // round_up = 0x3FFFFF: the smallest e with 6 * 2^e >= top, i.e. e + 127 = exponent field - 2, one more when the significand
 // is above 1.5 (the addition carries).  round_up = 0: e = floor(log2 top) - 2, with values above 6 * 2^e saturating.
+constexpr uint32_t kCoverRoundUp = 0x3FFFFFu;
 __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t m, uint32_t round_up) {
   const int s = static_cast<int>((m + round_up) >> 23) - 2;
   return m == 0u ? kScaleOne : static_cast<uint32_t>(max(s, 0));
@@ -163,9 +258,9 @@ __device__ __forceinline__ float scale_of(uint32_t s) {
   return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
 }
 
-// Eight scaled values to eight codes, the first in the low four bits: nearest, ties to the even pattern, saturating (the
+// Eight values, scaled, to eight codes, the first in the low four bits: nearest, ties to the even pattern, saturating (the
 // conversion instruction's own rule), and a zero magnitude always code 0 (it leaves the sign on small negative values).
-__device__ __forceinline__ uint32_t mx_encode_eight(const float (&v)[8], float inv) {
+__device__ __forceinline__ uint32_t mx_encode_eight(const float* v, float inv) {
   uint32_t w;
   asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
@@ -179,7 +274,7 @@ __device__ __forceinline__ uint32_t mx_encode_eight(const float (&v)[8], float i
   const uint32_t mag = w & 0x77777777u;
   return mag | (w & (mag + 0x77777777u) & 0x88888888u);      // a magnitude from 1 to 7 carries into bit 3
 }
-__device__ __forceinline__ void mx_decode_eight(uint32_t w, float scale, float (&v)[8]) {
+__device__ __forceinline__ void mx_decode_eight(uint32_t w, float scale, float* v) {
   uint32_t h[4];
   asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
       "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
@@ -196,29 +291,40 @@ __device__ __forceinline__ void mx_decode_eight(uint32_t w, float scale, float (
   }
 }
 
-// Eight scaled values to int8 codes in +-127, nearest even, NaN to 0: {codes 0-3, codes 4-7}.
-__device__ __forceinline__ uint2 i8_encode_eight(const float (&v)[8], float inv) {
-  uint32_t c[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = fminf(fmaxf(v[i] * inv, -127.0f), 127.0f);
-    c[i] = static_cast<uint32_t>(v[i] == v[i] ? __float2int_rn(t) : 0) & 0xFFu;
-  }
-  return make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
-}
-__device__ __forceinline__ void i8_decode_eight(uint2 w, float scale, float (&v)[8]) {
+// Four values, scaled, to int8 codes in +-127: nearest even, NaN to 0 (the conversion's rule, kept alive by the maximum that
+// hands NaN on), saturated as they are packed.
+__device__ __forceinline__ uint32_t i8_encode_four(const float* v, float inv) {
+  int c[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[i] = static_cast<float>(static_cast<int8_t>(w.x >> (8 * i))) * scale;
-    v[4 + i] = static_cast<float>(static_cast<int8_t>(w.y >> (8 * i))) * scale;
+    float t;
+    asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(t) : "f"(v[i] * inv));          // -127
+    c[i] = __float2int_rn(t);
   }
+  uint32_t lo, all;
+  asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, 0;" : "=r"(lo) : "r"(c[3]), "r"(c[2]));
+  asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(all) : "r"(c[1]), "r"(c[0]), "r"(lo));
+  return all;
+}
+// Four int8 codes to values: a byte with its sign bit turned is the low byte of the float 2^23 + 128 + code.
+__device__ __forceinline__ void i8_decode_four(uint32_t w, float scale, float* v) {
+  const uint32_t b = w ^ 0x80808080u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (__uint_as_float(__byte_perm(b, 0x4B000000u, 0x7440 + i)) - 8388736.0f) * scale;
 }
 
-// The scale bytes of four consecutive blocks, one held by every fourth lane of sixteen, as one word (valid in the first
-// of the sixteen lanes).
+// The scale bytes of four consecutive blocks of LANES lanes each as one word (valid in the first of their lanes).
+template <int LANES>
 __device__ __forceinline__ uint32_t gather_scale_word(uint32_t s) {
-  s |= __shfl_down_sync(0xffffffffu, s, 4) << 8;
-  return s | __shfl_down_sync(0xffffffffu, s, 8) << 16;
+  s |= __shfl_down_sync(0xffffffffu, s, LANES) << 8;
+  return s | __shfl_down_sync(0xffffffffu, s, 2 * LANES) << 16;
+}
+
+// Codes of a lane's E values in 4 bits.
+template <int E>
+__device__ __forceinline__ void mx_store_codes(uint8_t* p, const float (&v)[E], float inv) {
+  if constexpr (E == 8) *reinterpret_cast<uint32_t*>(p) = mx_encode_eight(v, inv);
+  else *reinterpret_cast<uint2*>(p) = make_uint2(mx_encode_eight(v, inv), mx_encode_eight(v + 8, inv));
 }
 
 // Where a row's scales go.
