@@ -8,6 +8,7 @@ fallback.
 """
 import ctypes
 import os
+import struct
 import subprocess
 import tempfile
 
@@ -220,11 +221,9 @@ def lib():
         L.qmx_linear_set_wait_limit.argtypes = [vp, ctypes.c_uint]
         L.qmx_linear_describe.argtypes = [vp, ctypes.c_char_p, sz]
         L.qmx_linear_destroy.argtypes = [vp]
-        L.qrmsnorm.argtypes = [ctypes.POINTER(qrmsnorm_args), vp]
-        L.qcache_write.argtypes = [ctypes.POINTER(qcache_desc), ctypes.POINTER(qcache_values), ctypes.POINTER(qcache_values),
-                                   ci, vp, ll, vp]
-        L.qcache_read.argtypes = [ctypes.POINTER(qcache_desc), vp, ll, ctypes.POINTER(qcache_values),
-                                  ctypes.POINTER(qcache_values), ci, vp]
+        L.qrmsnorm.argtypes = [vp, vp]                       # (structures as bytes or by reference)
+        L.qcache_write.argtypes = [vp, vp, vp, ci, vp, ll, vp]
+        L.qcache_read.argtypes = [vp, vp, ll, vp, vp, ci, vp]
         for name in ("qmx_quantize", "qmx_dequantize", "qmx_linear_create", "qmx_linear_run", "qmx_linear_status",
                      "qmx_linear_set_wait_limit", "qmx_linear_describe", "qmx_linear_destroy", "qrmsnorm", "qcache_write",
                      "qcache_read"):
@@ -652,85 +651,102 @@ def qquantize_bias(b, e_x, e_w):
 # ---------------------------------------------------------------------------------------------------------------
 # Operators for quantized language models.  These check the tensors they are given (device, type, shape, strides): a
 # tensor on another device than the current one, or one that is too small, is a ValueError before anything runs.
+# (Written for few Python operations a call: the smallest of these kernels take a microsecond or two.)
 # ---------------------------------------------------------------------------------------------------------------
-_types = None
+_types = {}
+_BYTES = ()
+_empty = None
+
+
+def _start():
+    """What the functions below look up, once."""
+    global _types, _BYTES, _empty
+    import torch
+    _stream()
+    _empty = torch.empty
+    _BYTES = (torch.uint8, torch.int8)
+    _types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
 
 
 def _type_of(dtype):
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+    if not _types:
+        _start()
     t = _types.get(dtype)
     if t is None:
         raise ValueError("float32, bfloat16 or float16 tensors are wanted, not %s" % dtype)
     return t
 
 
-def _on_device(*tensors):
-    """Every tensor (None: not given) on the current CUDA device."""
+def _device(*tensors):
+    """The current CUDA device, which every tensor (None: not given) must be on."""
     if _current_device is None:
-        _stream()
+        _start()
     dev = _current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != dev):
+        if t is not None and t.get_device() != dev:
             raise ValueError("the tensors must be on the current CUDA device (%d), not on %s" % (dev, t.device))
+    return dev
 
 
 def _rows(t, what):
     """Row stride of a 2-D tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    strides = t.stride()
+    if len(strides) != 2 or (strides[1] != 1 and t.shape[1] > 1):
         raise ValueError("%s must be 2-D with contiguous rows" % what)
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return strides[0] if t.shape[0] > 1 else max(strides[0], t.shape[1])
 
 
 def _bytes(t, count, what):
     """A contiguous tensor of at least `count` one-byte values."""
-    if t.element_size() != 1 or not t.is_contiguous() or t.numel() < count:
-        raise ValueError("%s must be a contiguous tensor of at least %d bytes" % (what, count))
+    if t.dtype not in _BYTES or t.numel() < count or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous uint8 (or int8) tensor of at least %d bytes" % (what, count))
 
 
 def _mx_size(rows, K, layout):
     """(bytes of codes in a row, bytes of all scales) of a microscaled tensor."""
-    blocks = -(-K // 32)
-    return blocks * 16, -(-rows // 128) * -(-blocks // 4) * 512 if layout == MX_TILES else rows * blocks
+    blocks = (K + 31) // 32
+    return blocks * 16, (rows + 127) // 128 * ((blocks + 3) // 4) * 512 if layout == MX_TILES else rows * blocks
 
 
 def qmx_quantize(x, rule=MX_COVER, layout=MX_TILES, codes=None, scales=None):
     """Float CUDA tensor [rows, K] (contiguous rows, any row stride) -> (codes [rows, ceil(K / 32) * 16] uint8, scales):
     microscaled 4-bit values in blocks of 32 along the row.  scales: uint8 [rows, ceil(K / 32)] for MX_ROWS, else the
     tiles that QMXLinear reads (flat)."""
-    import torch
+    type_ = _type_of(x.dtype)
     ld, (rows, K) = _rows(x, "x"), x.shape
     pitch, size = _mx_size(rows, K, layout)
     if codes is None:
-        codes = torch.empty((rows, pitch), dtype=torch.uint8, device=x.device)
+        codes = _empty((rows, pitch), dtype=_BYTES[0], device=x.device)
     if scales is None:
-        scales = torch.empty((rows, pitch // 16) if layout == MX_ROWS else (size,), dtype=torch.uint8, device=x.device)
-    _on_device(x, codes, scales)
+        scales = _empty((rows, pitch // 16) if layout == MX_ROWS else (size,), dtype=_BYTES[0], device=x.device)
+    dev = _device(x, codes, scales)
     _bytes(codes, rows * pitch, "codes")
     _bytes(scales, size, "scales")
-    if x.numel():
-        _check(lib().qmx_quantize(x.data_ptr(), _type_of(x.dtype), rows, K, ld, int(rule), int(layout), codes.data_ptr(),
-                                  scales.data_ptr(), _stream()))
+    if rows and K:
+        rc = (_lib or lib()).qmx_quantize(x.data_ptr(), type_, rows, K, ld, rule, layout, codes.data_ptr(), scales.data_ptr(), _raw_stream(dev))
+        if rc:
+            _check(rc)
     return codes, scales
 
 
 def qmx_dequantize(codes, scales, K, layout=MX_TILES, dtype=None, out=None):
     """Microscaled codes [rows, ...] and scales -> values [rows, K] of `dtype` (float32), or into `out`."""
-    import torch
     rows = codes.shape[0]
     if out is None:
+        import torch
         out = torch.empty((rows, K), dtype=dtype or torch.float32, device=codes.device)
-    elif tuple(out.shape) != (rows, K):
+    elif out.shape != (rows, K):
         raise ValueError("out must be [%d, %d]" % (rows, K))
+    type_ = _type_of(out.dtype)
     pitch, size = _mx_size(rows, K, layout)
-    _on_device(codes, scales, out)
+    dev = _device(codes, scales, out)
     _bytes(codes, rows * pitch, "codes")
     _bytes(scales, size, "scales")
-    if out.numel():
-        _check(lib().qmx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, int(K), int(layout), out.data_ptr(),
-                                    _type_of(out.dtype), _rows(out, "out"), _stream()))
+    if rows and K:
+        rc = (_lib or lib()).qmx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, K, layout, out.data_ptr(), type_, _rows(out, "out"),
+                                            _raw_stream(dev))
+        if rc:
+            _check(rc)
     return out
 
 
@@ -740,15 +756,15 @@ class QMXLinear:
 
     def __init__(self, w_codes, w_scales, N, K, bias=None, relu=0, dtype=None):
         import torch
-        pitch, size = _mx_size(N, K, MX_TILES)
-        _on_device(w_codes, w_scales, bias)
-        _bytes(w_codes, N * pitch, "w_codes")
+        self.dtype = dtype or torch.bfloat16
+        self.desc = qmx_linear_desc(N=N, K=K, relu=int(relu), type=_type_of(self.dtype))
+        self._pitch, size = _mx_size(N, K, MX_TILES)
+        _device(w_codes, w_scales, bias)
+        _bytes(w_codes, N * self._pitch, "w_codes")
         _bytes(w_scales, size, "w_scales")
         if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != N):
             raise ValueError("the bias must be %d contiguous float32 values" % N)
-        self.dtype = dtype or torch.bfloat16
-        self.desc = qmx_linear_desc(N=N, K=K, relu=int(relu), type=_type_of(self.dtype))
-        self.N, self.K, self._pitch = N, K, pitch
+        self.N, self.K, self._tiles = N, K, (K + 127) // 128 * 512
         self._keep = (w_codes, w_scales, bias)
         self.handle = ctypes.c_void_p()
         _check(lib().qmx_linear_create(ctypes.byref(self.handle), ctypes.byref(self.desc), w_codes.data_ptr(), w_scales.data_ptr(),
@@ -759,15 +775,14 @@ class QMXLinear:
         """x_codes [tokens, ...], x_scales in tiles -> y [tokens, N] (contiguous rows).  Asynchronous on the current stream."""
         tokens = x_codes.shape[0]
         if y is None:
-            import torch
-            y = torch.empty((tokens, self.N), dtype=self.dtype, device=x_codes.device)
-        _on_device(x_codes, x_scales, y)
+            y = _empty((tokens, self.N), dtype=self.dtype, device=x_codes.device)
+        dev = _device(x_codes, x_scales, y)
         _bytes(x_codes, tokens * self._pitch, "x_codes")
-        _bytes(x_scales, -(-tokens // 128) * -(-self._pitch // 64) * 512, "x_scales")
+        _bytes(x_scales, (tokens + 127) // 128 * self._tiles, "x_scales")
         if y.dtype != self.dtype or y.shape != (tokens, self.N):
             raise ValueError("y must be [%d, %d] of %s" % (tokens, self.N, self.dtype))
         if tokens:
-            rc = self._run(self.handle, x_codes.data_ptr(), x_scales.data_ptr(), tokens, y.data_ptr(), _rows(y, "y"), _stream())
+            rc = self._run(self.handle, x_codes.data_ptr(), x_scales.data_ptr(), tokens, y.data_ptr(), _rows(y, "y"), _raw_stream(dev))
             if rc:
                 _check(rc)
         return y
@@ -795,35 +810,46 @@ class QMXLinear:
             pass
 
 
+# qrmsnorm_args and qcache_values as bytes: packing one takes a third of the time of filling in a ctypes structure.
+_NORM_ARGS = struct.Struct("@4P2i4qd3i4x2P")
+_CACHE_VALUES = struct.Struct("@P2q")
+
+
 def qrmsnorm(x, gain, eps, residual=None, sum_out=None, out=NORM_I8, e=0, layout=MX_TILES, codes=None, scales=None):
     """Residual addition, root-mean-square norm and conversion of x [rows, C]: (codes, scales) with int8 codes at
     exponent e (NORM_I8; scales None), int8 codes and a scale byte per row (NORM_I8_ROWS), or microscaled 4 bits
     (NORM_MX).  sum_out receives x + residual and may be x or residual itself."""
-    import torch
-    ld, (rows, C) = _rows(x, "x"), x.shape
-    for t, what in ((residual, "residual"), (sum_out, "sum_out")):
-        if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
-            raise ValueError("%s must be like x" % what)
-    if gain.dtype != x.dtype or gain.shape != (C,) or not gain.is_contiguous():
+    dtype, shape = x.dtype, x.shape
+    type_, ld, (rows, C) = _type_of(dtype), _rows(x, "x"), shape
+    ld_residual = ld_sum = residual_at = sum_at = 0
+    if residual is not None:
+        if residual.dtype != dtype or residual.shape != shape:
+            raise ValueError("residual must be like x")
+        ld_residual, residual_at = _rows(residual, "residual"), residual.data_ptr()
+    if sum_out is not None:
+        if sum_out.dtype != dtype or sum_out.shape != shape:
+            raise ValueError("sum_out must be like x")
+        ld_sum, sum_at = _rows(sum_out, "sum_out"), sum_out.data_ptr()
+    if gain.dtype != dtype or gain.shape != (C,) or not gain.is_contiguous():
         raise ValueError("the gain must be %d contiguous values of x's type" % C)
     pitch, size = _mx_size(rows, C, layout) if out == NORM_MX else (C, rows)
     if codes is None:
-        codes = torch.empty((rows, pitch), dtype=torch.uint8 if out == NORM_MX else torch.int8, device=x.device)
+        codes = _empty((rows, pitch), dtype=_BYTES[0 if out == NORM_MX else 1], device=x.device)
+    scales_at = 0
     if out == NORM_I8:
         scales = None
-    elif scales is None:
-        shape = (rows, pitch // 16) if out == NORM_MX and layout == MX_ROWS else (size,)
-        scales = torch.empty(shape, dtype=torch.uint8, device=x.device)
-    _on_device(x, gain, residual, sum_out, codes, scales)
-    _bytes(codes, rows * pitch, "codes")
-    if scales is not None:
+    else:
+        if scales is None:
+            scales = _empty((rows, pitch // 16) if out == NORM_MX and layout == MX_ROWS else (size,), dtype=_BYTES[0], device=x.device)
         _bytes(scales, size, "scales")
-    if x.numel():
-        a = qrmsnorm_args(x.data_ptr(), _dev(residual), gain.data_ptr(), _dev(sum_out), _type_of(x.dtype), C, rows, ld,
-                          _rows(residual, "residual") if residual is not None else 0,
-                          _rows(sum_out, "sum_out") if sum_out is not None else 0, float(eps), int(out), int(e), int(layout),
-                          codes.data_ptr(), _dev(scales))
-        _check(lib().qrmsnorm(ctypes.byref(a), _stream()))
+        scales_at = scales.data_ptr()
+    dev = _device(x, gain, residual, sum_out, codes, scales)
+    _bytes(codes, rows * pitch, "codes")
+    if rows and C:
+        rc = (_lib or lib()).qrmsnorm(_NORM_ARGS.pack(x.data_ptr(), residual_at, gain.data_ptr(), sum_at, type_, C, rows, ld, ld_residual, ld_sum,
+                                                      eps, out, e, layout, codes.data_ptr(), scales_at), _raw_stream(dev))
+        if rc:
+            _check(rc)
     return codes, scales
 
 
@@ -835,7 +861,9 @@ class QCache:
         slots, heads = k_codes.shape[:2]
         D = k_codes.shape[2] if D is None else D
         blocks = -(-D // 32)
-        _on_device(k_codes, k_scales, v_codes, v_scales)
+        _device(k_codes, k_scales, v_codes, v_scales)
+        if not _types:
+            _start()
         if (v_codes is None) != (v_scales is None):
             raise ValueError("v_codes and v_scales belong together")
         for c, s in ((k_codes, k_scales), (v_codes, v_scales)):
@@ -846,6 +874,7 @@ class QCache:
         self._keep = (k_codes, k_scales, v_codes, v_scales)
         self.desc = qcache_desc(int(fmt), heads, D, slots, _dev(k_codes), _dev(k_scales), _dev(v_codes), _dev(v_scales))
         self._desc = ctypes.byref(self.desc)
+        self._write, self._read = lib().qcache_write, lib().qcache_read
 
     @classmethod
     def empty(cls, slots, heads, D, fmt=CACHE_I8, values=True, device="cuda"):
@@ -859,29 +888,31 @@ class QCache:
     k_codes, k_scales, v_codes, v_scales = (property(lambda self, i=i: self._keep[i]) for i in range(4))
 
     def _values(self, t, rows, dtype):
-        if t.dim() != 3 or t.shape != (rows, self.heads, self.D) or t.dtype != dtype or (t.stride(2) != 1 and self.D > 1):
+        strides = t.stride()
+        if t.dtype != dtype or t.shape != (rows, self.heads, self.D) or (strides[2] != 1 and self.D > 1):
             raise ValueError("keys and values must be [%d, %d, %d] of one type with contiguous heads" % (rows, self.heads, self.D))
-        return qcache_values(t.data_ptr(), t.stride(0), t.stride(1))
+        return _CACHE_VALUES.pack(t.data_ptr(), strides[0], strides[1])
 
     def _args(self, slots, k, v):
         if slots.dim() != 1 or not slots.is_contiguous() or slots.element_size() != 8 or slots.is_floating_point():
             raise ValueError("slots must be a contiguous 1-D int64 tensor")
         if (v is None) != (self._keep[2] is None):
             raise ValueError("the cache holds %s" % ("keys alone" if v is not None else "keys and values"))
-        _on_device(slots, k, v)
-        rows = slots.shape[0]
-        keys = self._values(k, rows, k.dtype)
-        return rows, _type_of(k.dtype), ctypes.byref(keys), ctypes.byref(self._values(v, rows, k.dtype)) if v is not None else None
+        dtype, rows = k.dtype, slots.shape[0]
+        return (rows, _type_of(dtype), self._values(k, rows, dtype), None if v is None else self._values(v, rows, dtype),
+                _raw_stream(_device(slots, k, v)))
 
     def write(self, slots, k, v=None):
         """Rows of k (and v) [rows, heads, D] into the slots; rows whose slot is outside the cache are skipped."""
-        rows, dtype, keys, values = self._args(slots, k, v)
-        if rows:
-            _check(lib().qcache_write(self._desc, keys, values, dtype, slots.data_ptr(), rows, _stream()))
+        rows, type_, keys, values, stream = self._args(slots, k, v)
+        rc = self._write(self._desc, keys, values, type_, slots.data_ptr(), rows, stream) if rows else 0
+        if rc:
+            _check(rc)
 
     def read(self, slots, k, v=None):
         """The slots' keys (and values) into k (and v) [rows, heads, D]; rows whose slot is outside the cache stay as they are."""
-        rows, dtype, keys, values = self._args(slots, k, v)
-        if rows:
-            _check(lib().qcache_read(self._desc, slots.data_ptr(), rows, keys, values, dtype, _stream()))
+        rows, type_, keys, values, stream = self._args(slots, k, v)
+        rc = self._read(self._desc, slots.data_ptr(), rows, keys, values, type_, stream) if rows else 0
+        if rc:
+            _check(rc)
         return k, v

@@ -1,8 +1,8 @@
 // Quantized caches: the values of a token's heads are converted as they are written to their slot, and read back from
 // any list of slots.  A head's D values are one group: int8 with an exponent for the group, or microscaled 4 bits.  Bound by
 // HBM on long lists and by the launch on short ones: keys and values go in one launch, a head takes LANES lanes with V
-// pieces of 32 bytes each, and a group of lanes has kCacheUnroll heads in flight (their slots, codes and scales are a chain
-// of dependent loads).
+// pieces of 32 bytes each, and a group of lanes has kCacheUnroll heads in flight and the slots of the next ones on their
+// way (slot, then codes and scales, are dependent loads).
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
@@ -11,18 +11,7 @@ namespace qc {
 
 enum : int { CACHE_I8 = 0, CACHE_MX = 1 };
 constexpr int kCacheThreads = 256;
-#ifndef CWU
-#define CWU 2
-#endif
-#ifndef CRU
-#define CRU 4
-#endif
-#ifndef CWB
-#define CWB 4
-#endif
-#ifndef CRB
-#define CRB 4
-#endif
+constexpr int kCacheUnroll = 2, kCacheBlocks = 4;
 
 struct CacheSide {
   uint8_t* codes;
@@ -46,14 +35,19 @@ struct CacheItem {
   bool valid, second;        // second: of the values, not the keys
   size_t values, group;      // element offset of the head's values; index of (slot, head)
 };
-__device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, int u) {
-  CacheItem c = {false, false, 0, 0};
-  if (u >= a.items) return c;
+// The slot of item u (-1 behind the last); items are (row, side, head), head fastest.
+__device__ __forceinline__ long long cache_slot(const CacheArgs& a, int u) {
+  if (u >= a.items) return -1;
+  int h;
+  const int rs = a.fd_heads.divmod(u, &h);
+  return __ldg(a.slots + (a.sides == 2 ? rs >> 1 : rs));
+}
+__device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, int u, long long slot) {
+  CacheItem c;
   int h;
   const int rs = a.fd_heads.divmod(u, &h);
   const int row = a.sides == 2 ? rs >> 1 : rs;
   c.second = a.sides == 2 && (rs & 1);
-  const long long slot = __ldg(a.slots + row);
   c.valid = slot >= 0 && slot < a.num_slots && QC_IN(slot, a.num_slots);
   c.values = static_cast<size_t>(row * (c.second ? a.side[1].token : a.side[0].token) + h * (c.second ? a.side[1].head : a.side[0].head));
   c.group = static_cast<size_t>(slot) * a.heads + h;
@@ -72,9 +66,9 @@ __device__ __forceinline__ T* cache_values(const CacheArgs& a, const CacheItem& 
 
 // LANES lanes a head, V pieces a lane.
 template <typename T, int FMT, int LANES, int V, bool ANY>
-__global__ void __launch_bounds__(kCacheThreads, V == 1 ? CWB : 1)
+__global__ void __launch_bounds__(kCacheThreads, V == 1 ? kCacheBlocks : 1)
 cache_write_kernel(const CacheArgs a) {
-  constexpr int E = Piece<T>::E, U = V == 1 ? CWU : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
+  constexpr int E = Piece<T>::E, U = V == 1 ? kCacheUnroll : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
   __shared__ uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
@@ -83,11 +77,16 @@ cache_write_kernel(const CacheArgs a) {
   uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
   // the lanes of a warp run the same number of rounds
   const int warp_first = (threadIdx.x >> 5) * kPerWarp, mine = (threadIdx.x & 31) / LANES;
+  long long slot[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, blockIdx.x * kPerBlock + warp_first + j * step + mine);
   for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += U * step) {
     CacheItem c[U];
     Piece<T> x[U][V];
 #pragma unroll
-    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine);
+    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine, slot[j]);
+#pragma unroll
+    for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, base + (U + j) * step + mine);
 #pragma unroll
     for (int j = 0; j < U; ++j)
 #pragma unroll
@@ -142,9 +141,9 @@ cache_write_kernel(const CacheArgs a) {
 }
 
 template <typename T, int FMT, int LANES, int V, bool ANY>
-__global__ void __launch_bounds__(kCacheThreads, V == 1 ? CRB : 1)
+__global__ void __launch_bounds__(kCacheThreads, V == 1 ? kCacheBlocks : 1)
 cache_read_kernel(const CacheArgs a) {
-  constexpr int E = Piece<T>::E, U = V == 1 ? CRU : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
+  constexpr int E = Piece<T>::E, U = V == 1 ? kCacheUnroll : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
   __shared__ uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
@@ -152,11 +151,16 @@ cache_read_kernel(const CacheArgs a) {
   const int step = gridDim.x * kPerBlock;
   uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
   const int warp_first = (threadIdx.x >> 5) * kPerWarp, mine = (threadIdx.x & 31) / LANES;
+  long long slot[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, blockIdx.x * kPerBlock + warp_first + j * step + mine);
   for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += U * step) {
     CacheItem c[U];
     uint32_t w[U][V][E / 4], sb[U][V];                      // (4-bit codes: the first half)
 #pragma unroll
-    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine);
+    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine, slot[j]);
+#pragma unroll
+    for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, base + (U + j) * step + mine);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const uint8_t* codes = cache_codes(a, c[j]);

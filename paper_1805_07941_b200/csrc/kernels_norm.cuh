@@ -177,11 +177,10 @@ __device__ __forceinline__ void norm_store_mx(const NormArgs<T>& a, const NormPl
   constexpr int E = Piece<T>::E, kBlockLanes = kMxBlock / E;
   const int col = first + at.lane * E;
   const uint32_t s = mx_scale_byte(finite_top<kBlockLanes>(y, top_bits(y)), kCoverRoundUp);
-  const uint32_t word = gather_scale_word<kBlockLanes>(s);
   const int padded = a.scales.blocks * kMxBlock;
-  if (!at.valid || !QC_IN(at.row, a.rows) || col >= padded) return;
-  mx_store_codes(a.codes + at.row * static_cast<size_t>(padded / 2) + col / 2, y, inverse_scale(s));
-  if ((col & 127) == 0) store_scale_word(a.scales, at.row, col >> 7, word);
+  const bool here = at.valid && col < padded && QC_IN(at.row, a.rows);
+  store_scale<kBlockLanes>(a.scales, at.row, col, s, here);
+  if (here) mx_store_codes(a.codes + at.row * static_cast<size_t>(padded / 2) + col / 2, y, inverse_scale(s));
 }
 
 // Scale words of the rows that fill up the last tile of 128, by `blocks` blocks of which this is number `block`.

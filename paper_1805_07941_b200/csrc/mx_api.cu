@@ -90,13 +90,14 @@ qc::MxGrid mx_grid(long long rows, long long rows_out, int K, long long ld, int 
   const int lanes = qc::mx_blocks(K) * (qc::kMxBlock / E);
   qc::MxGrid g = {};
   g.lanes_x = 128 / E;                                     // of a scale word
-  g.log_x = E == 8 ? 4 : 3;
-  while (g.lanes_x < qc::kMxThreads && g.lanes_x < lanes) { g.lanes_x *= 2; ++g.log_x; }
+  while (g.lanes_x < qc::kMxThreads && g.lanes_x < lanes) g.lanes_x *= 2;
+  while (g.lanes_x > 32 && ((lanes + g.lanes_x - 1) / g.lanes_x * g.lanes_x - lanes) * 8 > lanes) g.lanes_x /= 2;   // few lanes behind the row's end
+  while ((1 << g.log_x) < g.lanes_x) ++g.log_x;
   g.rows = static_cast<size_t>(rows); g.rows_out = static_cast<size_t>(rows_out); g.K = K; g.ld = static_cast<size_t>(ld);
   g.how = reach(values, type, ld);
   const long long per_block = qc::kMxThreads / g.lanes_x;
   grid->x = static_cast<unsigned int>((lanes + g.lanes_x - 1) / g.lanes_x);
-  const long long most = std::max(1ll, 148ll * 16 / grid->x);
+  const long long most = std::max(1ll, 148ll * qc::kMxBlocks / grid->x);   // (all at once, as many rows each)
   grid->y = static_cast<unsigned int>(std::min({(rows_out + per_block - 1) / per_block, most, 65535ll}));
   return g;
 }
@@ -415,13 +416,14 @@ int launch_norm(const qc::NormArgs<T>& a, int G, int warps, cudaStream_t st) {
   const unsigned int y = warps == 1 ? 4 : 1;
   const size_t per_block = static_cast<size_t>(y) * (32 / G);
   const unsigned int blocks = static_cast<unsigned int>((a.rows + per_block - 1) / per_block);
-  const auto kernel = a.how == qc::ROWS_ANY ? qc::rmsnorm_kernel<T, OUT, V, true> : qc::rmsnorm_kernel<T, OUT, V, false>;
+  auto kernel = qc::rmsnorm_kernel<T, OUT, V, false>;
+  if constexpr (V <= 2) kernel = a.how == qc::ROWS_ANY ? qc::rmsnorm_kernel<T, OUT, V, true> : kernel;
   CUDA_TRY(launch_chained(kernel, dim3(blocks + pad_blocks<OUT>(a)), dim3(32 * warps, y), norm_stages<T, OUT>(a, warps * static_cast<int>(y)), st, a, G, blocks));
   return QCONV_OK;
 }
 
 // A row's values in registers: pieces of 32 bytes, one a lane for few rows (the more warps, the shorter the chain of a
-// thread), two or four for many.
+// thread), two or four for many (unaligned ones only up to two: they pass through registers one by one first).
 template <typename T, int OUT>
 int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
   constexpr int E = qc::Piece<T>::E;
@@ -434,7 +436,7 @@ int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
   }
   if (lanes <= 1024 && a.rows < 512) return launch_norm<T, OUT, 1>(a, 32, warps(1), st);
   if (lanes <= 1024) return launch_norm<T, OUT, 2>(a, 32, warps(2), st);
-  if (lanes <= 2048) return launch_norm<T, OUT, 4>(a, 32, warps(4), st);
+  if (lanes <= 2048 && a.how != qc::ROWS_ANY) return launch_norm<T, OUT, 4>(a, 32, warps(4), st);
   const auto kernel = a.how == qc::ROWS_ANY ? qc::rmsnorm_long_kernel<T, OUT, true> : qc::rmsnorm_long_kernel<T, OUT, false>;
   const unsigned int blocks = static_cast<unsigned int>(a.rows);
   CUDA_TRY(launch_chained(kernel, dim3(blocks + pad_blocks<OUT>(a)), dim3(32 * qc::kNormMaxWarps), norm_stages<T, OUT>(a, qc::kNormMaxWarps), st, a, blocks));

@@ -313,13 +313,6 @@ __device__ __forceinline__ void i8_decode_four(uint32_t w, float scale, float* v
   for (int i = 0; i < 4; ++i) v[i] = (__uint_as_float(__byte_perm(b, 0x4B000000u, 0x7440 + i)) - 8388736.0f) * scale;
 }
 
-// The scale bytes of four consecutive blocks of LANES lanes each as one word (valid in the first of their lanes).
-template <int LANES>
-__device__ __forceinline__ uint32_t gather_scale_word(uint32_t s) {
-  s |= __shfl_down_sync(0xffffffffu, s, LANES) << 8;
-  return s | __shfl_down_sync(0xffffffffu, s, 2 * LANES) << 16;
-}
-
 // Codes of a lane's E values in 4 bits.
 template <int E>
 __device__ __forceinline__ void mx_store_codes(uint8_t* p, const float (&v)[E], float inv) {
@@ -334,18 +327,23 @@ struct MxScales {
   int blocks, tiles_k;
   size_t extent;        // bytes of the whole array
 };
-// The word of blocks 4 t .. 4 t + 3 of row r; in tiles also the bytes behind the row's last block (a byte of 2^0 each).
+// The word of blocks 4 t .. 4 t + 3 of row r, in tiles (with the bytes behind the row's last block: a byte of 2^0 each).
 __device__ __forceinline__ void store_scale_word(const MxScales& s, size_t r, int t, uint32_t word) {
-  if (s.tiles) {
-    const size_t at = mx_tile_word(r, t, s.tiles_k);
-    if (QC_IN(at + 3, s.extent)) *reinterpret_cast<uint32_t*>(s.bytes + at) = word;
-  } else {
-    const size_t at = r * static_cast<size_t>(s.blocks) + 4 * t;
-    const int n = min(4, s.blocks - 4 * t);
-    if (!QC_IN(at + n - 1, s.extent)) return;
-    if (n == 4 && (reinterpret_cast<uintptr_t>(s.bytes + at) & 3) == 0) *reinterpret_cast<uint32_t*>(s.bytes + at) = word;
-    else
-      for (int i = 0; i < n; ++i) s.bytes[at + i] = static_cast<uint8_t>(word >> (8 * i));
+  const size_t at = mx_tile_word(r, t, s.tiles_k);
+  if (QC_IN(at + 3, s.extent)) *reinterpret_cast<uint32_t*>(s.bytes + at) = word;
+}
+// The scale byte s of the block of which this lane's values, from column `col` of row r on, are a part.  Every lane of a warp
+// calls it (`here`: the lane has values or their padding); LANES lanes a block.
+template <int LANES>
+__device__ __forceinline__ void store_scale(const MxScales& scales, size_t r, int col, uint32_t s, bool here) {
+  if (scales.tiles) {
+    // four blocks at once
+    s |= __shfl_down_sync(0xffffffffu, s, LANES) << 8;
+    s |= __shfl_down_sync(0xffffffffu, s, 2 * LANES) << 16;
+    if (here && (col & 127) == 0) store_scale_word(scales, r, col >> 7, s);
+  } else if (here && (col & (kMxBlock - 1)) == 0) {
+    const size_t at = r * static_cast<size_t>(scales.blocks) + col / kMxBlock;
+    if (QC_IN(at, scales.extent)) scales.bytes[at] = static_cast<uint8_t>(s);
   }
 }
 

@@ -26,6 +26,14 @@ def test_structs_match_the_header(name):
     assert fields == [n for n, _ in getattr(binding, name)._fields_]
 
 
+def test_structs_as_bytes_have_the_structures_layout():
+    for packed, structure in ((binding._NORM_ARGS, binding.qrmsnorm_args), (binding._CACHE_VALUES, binding.qcache_values)):
+        names = [n for n, _ in structure._fields_]
+        assert packed.size == ctypes.sizeof(structure)
+        s = structure.from_buffer_copy(packed.pack(*range(1, len(names) + 1)))
+        assert [int(getattr(s, n)) for n in names] == list(range(1, len(names) + 1))
+
+
 def test_sizes(lib):
     assert lib.qmx_code_bytes(3, 33) == 3 * 32 and lib.qmx_scale_bytes(3, 33, 0) == 6
     assert lib.qmx_scale_bytes(129, 129, 1) == 2 * 2 * 512
