@@ -1,12 +1,15 @@
 // Products of microscaled 4-bit operands (kernel_mx_gemm.cuh has the mathematics, layouts and orientation) on PAIRS of SMs:
-// a cluster of two CTAs computes tiles of 256 output channels x 256 tokens with tcgen05.mma.cta_group::2.  Each CTA loads
-// the codes of its own 128 channels and of half the tokens, the scales of its channels and of all 256 tokens; per
+// a cluster of two CTAs computes tiles of 256 output channels x 192 tokens with tcgen05.mma.cta_group::2.  Each CTA loads
+// the codes of its own 128 channels and of half the tokens, the scales of its channels and of all the tokens; per
 // multiply-add that is half the operand bytes of a 128 x 128 tile, which is what bounds long prompts.
 //
-// The kernel is persistent, and the epilogue of a tile runs beside the products of the next.  Two accumulators of 256
-// columns and the scales do not fit the 512 columns of tensor memory; the accumulators therefore overlap: tile i uses
-// columns 0 .. 255 or 208 .. 463 in turn, scales 464 .. 511.  The epilogue drains the shared 48 columns first and then
-// lets the next tile start; the rest of the tile is long drained when the tile after that one reaches it.
+// The kernel is persistent, and the epilogue of a tile runs beside the products of the next: two accumulators of 192
+// columns and a place for the scales of each ring stage fill the 512 columns of tensor memory.  (Tiles of 256 tokens, whose
+// accumulators have to overlap, lose about 2000 cycles between two tiles: 8192 x 8192 x 8192 220 us instead of 194.)  A
+// token tile may begin in the middle of a scale tile: its scales then start two columns on.
+//
+// Outputs whose rows are 16-byte aligned and a multiple of 16 bytes long leave through shared memory and bulk stores,
+// whole rows of 128 channels; stored by the lanes a token is four pieces of 32 channels.
 //
 // Roles per CTA (320 threads): warp 0 lane 0 issues the loads, warp 1 owns tensor memory (lane 0 of the first CTA issues
 // scale copies and MMAs for both), warps 2-9 are the epilogue: tensor-memory lanes warp % 4, one half of the columns each.
@@ -39,7 +42,17 @@ struct MxPairShared {
   uint32_t tmem_base;
   volatile int abort_flag;
 };
-constexpr size_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStage + sizeof(MxPairShared);
+constexpr int kMxPairChunks = kMxPairTokens / 64;                         // of 32 tokens, in each half of the columns
+// Staged outputs of one half of the columns: a buffer holds kBatch chunks of [32 tokens][128 channels]: a whole tile of a
+// 16-bit type, or a chunk of float32 at a time in two buffers.
+template <typename Y> struct MxPairOut {
+  static constexpr uint32_t kChunkBytes = 32 * 128 * sizeof(Y);
+  static constexpr int kBatch = sizeof(Y) == 2 ? kMxPairChunks : 1, kBuffers = sizeof(Y) == 2 ? 1 : 2;
+  static constexpr uint32_t kBufferBytes = kBatch * kChunkBytes;
+  static constexpr uint32_t kBytes = 2 * kBuffers * kBufferBytes;
+};
+template <typename Y, bool STAGED>
+constexpr size_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStage + (STAGED ? MxPairOut<Y>::kBytes : 0) + sizeof(MxPairShared);
 
 namespace ptx {
 __device__ __forceinline__ void mma_mxf4_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem,
@@ -50,6 +63,21 @@ __device__ __forceinline__ void mma_mxf4_pair(uint32_t d_tmem, uint64_t a_desc, 
       "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate)
       : "memory");
+}
+// Shared-memory tile -> global tensor, clipped to its extent.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
+// All but the N most recent groups of this thread's bulk stores have read their source; all of them are complete.
+template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void sts_u16(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(static_cast<unsigned short>(v)) : "memory");
+}
+__device__ __forceinline__ void sts_u32(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // Each CTA's scale tile at this shared-memory offset to its own tensor memory.
 __device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t desc) {
@@ -68,6 +96,52 @@ __device__ __forceinline__ bool mx_wait_hint(uint32_t bar, uint32_t parity, unsi
   return false;
 }
 
+// Barriers of the four epilogue warps of one half of the columns; the second one also tells whether any of them failed.
+__device__ __forceinline__ void mx_half_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool mx_half_vote(int id, bool failed) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred pin, pout;\n\t"
+      "setp.ne.u32 pin, %1, 0;\n\t"
+      "bar.red.or.pred pout, %2, 128, pin;\n\t"
+      "selp.u32 %0, 1, 0, pout;\n\t}"
+      : "=r"(any) : "r"(failed ? 1u : 0u), "r"(id) : "memory");
+  return any != 0;
+}
+
+// Two values rounded to 16 bits, the first one low; negative ones to 0 with RELU (NaN stays).
+template <bool RELU> __device__ __forceinline__ uint32_t mx_pack(float a, float b, __nv_bfloat16) {
+  uint32_t r;
+  if constexpr (RELU) asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+template <bool RELU> __device__ __forceinline__ uint32_t mx_pack(float a, float b, __half) {
+  uint32_t r;
+  if constexpr (RELU) asm("cvt.rn.relu.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+// A lane's sums of BATCH chunks, from chunk k0 on, to its channel of the staged rows.
+template <typename Y, int BATCH, bool RELU>
+__device__ __forceinline__ void mx_stage(uint32_t mine, const uint32_t (&acc)[kMxPairChunks][32], int k0, float b) {
+#pragma unroll
+  for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      const float v0 = __uint_as_float(acc[k0 + k][i]) + b, v1 = __uint_as_float(acc[k0 + k][i + 1]) + b;
+      const uint32_t row = static_cast<uint32_t>(k * 32 + i) * 128 * sizeof(Y);
+      if constexpr (sizeof(Y) == 2) {
+        const uint32_t w = mx_pack<RELU>(v0, v1, Y());
+        ptx::sts_u16(mine + row, w);
+        ptx::sts_u16(mine + row + 128 * sizeof(Y), w >> 16);
+      } else {
+        ptx::sts_u32(mine + row, __float_as_uint(RELU && v0 < 0.0f ? 0.0f : v0));
+        ptx::sts_u32(mine + row + 128 * sizeof(Y), __float_as_uint(RELU && v1 < 0.0f ? 0.0f : v1));
+      }
+    }
+}
+
 // Tile u of the walk: groups of eight token tiles, within a group channel tile after channel tile, so that pairs that run
 // side by side share both operands in L2.
 struct MxPairTile { int n0, t0; };
@@ -79,14 +153,16 @@ __device__ __forceinline__ MxPairTile mx_pair_tile(const MxGemmParams& p, int u)
   return {tn * 256, (8 * g + in - tn * wide) * kMxPairTokens};
 }
 
-template <typename Y>
+template <typename Y, bool STAGED>
 __global__ void __launch_bounds__(kMxPairThreads, 1)
 mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                    const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const MxGemmParams prm,
-                    const float* __restrict__ bias, Y* __restrict__ y, int* status, unsigned int wait_limit) {
+                    const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs,
+                    const __grid_constant__ CUtensorMap map_y, const MxGemmParams prm, const float* __restrict__ bias, Y* __restrict__ y,
+                    int* status, unsigned int wait_limit) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  MxPairShared* sh = reinterpret_cast<MxPairShared*>(ring + kMxPairStages * kMxPairStage);
+  uint8_t* out = ring + kMxPairStages * kMxPairStage;        // STAGED: [half][buffer][chunk][32 tokens][128 channels]
+  MxPairShared* sh = reinterpret_cast<MxPairShared*>(out + (STAGED ? MxPairOut<Y>::kBytes : 0));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
   const int pair = static_cast<int>(blockIdx.x) >> 1, pairs = static_cast<int>(gridDim.x) >> 1;
@@ -220,35 +296,63 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     // -------------------------------------------------------------------- epilogue: lanes 32 (warp % 4) .., half the columns
     const int quad = warp & 3, half = (warp - 2) >> 2;
     const uint32_t free0 = ptx::map_to_cta(ptx::smem_u32(&sh->acc_free[0]), 0u);
+    using Out = MxPairOut<Y>;
+    const uint32_t my_out = ptx::smem_u32(out) + static_cast<uint32_t>(half) * Out::kBuffers * Out::kBufferBytes;
+    const bool storer = quad == ((2 + 4 * half) & 3) && lane == 0;         // of this half
+    int buffer = 0;
     int tiles = 0;
     for (int u = pair; u < total; u += pairs, ++tiles) {
       const MxPairTile tile = mx_pair_tile(prm, u);
-      const int n = tile.n0 + static_cast<int>(rank) * 128 + quad * 32 + lane;
+      const int n0 = tile.n0 + static_cast<int>(rank) * 128, n = n0 + quad * 32 + lane;
       const float b = bias != nullptr && n < prm.N ? __ldg(bias + n) : 0.0f;
       const int buf = tiles & 1;
       const bool ok = mx_wait_hint(ptx::smem_u32(&sh->acc_full[buf]), static_cast<uint32_t>(tiles >> 1) & 1u, wait_limit, &sh->abort_flag, status);
-      if (!__all_sync(0xffffffffu, ok)) break;
+      // (staged: the four warps of a half meet at barriers below, so they leave together)
+      if (STAGED ? mx_half_vote(1 + half, !ok) : !__all_sync(0xffffffffu, ok)) break;
       ptx::tc_fence_after();
-      const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16) + (buf ? kMxPairTokens : 0);
-#pragma unroll 1
-      for (int c0 = half * (kMxPairTokens / 2); c0 < (half + 1) * (kMxPairTokens / 2); c0 += 32) {
-        uint32_t acc[32];
-        ptx::tmem_ld_32x32(lanes + c0, acc);
-        ptx::tmem_ld_wait();
-        Y* p = y + static_cast<size_t>(tile.t0 + c0) * prm.ld + n;
-        const int cols = n < prm.N ? prm.T - (tile.t0 + c0) : 0;
+      const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16) + (buf ? kMxPairTokens : 0) + half * (kMxPairTokens / 2);
+      // All of the warp's columns first, then the accumulator is given back.  The arrival is a relaxed one: what it says is
+      // that the reads above are complete (tcgen05.wait::ld), and no write of this thread has to be seen by whoever waits for
+      // it; a release would wait for the stores of the tile before.
+      uint32_t acc[kMxPairChunks][32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float v = __uint_as_float(acc[i]) + b;
-          if (prm.relu) v = v < 0.0f ? 0.0f : v;
-          if (i < cols) *p = from_float<Y>(v);
+      for (int k = 0; k < kMxPairChunks; ++k) ptx::tmem_ld_32x32(lanes + 32 * k, acc[k]);
+      ptx::tmem_ld_wait();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster_relaxed(free0 + 8u * static_cast<uint32_t>(buf));
+      const int t0 = tile.t0 + half * (kMxPairTokens / 2);
+      if constexpr (STAGED) {
+#pragma unroll
+        for (int k0 = 0; k0 < kMxPairChunks; k0 += Out::kBatch) {
+          const uint32_t to = my_out + static_cast<uint32_t>(buffer) * Out::kBufferBytes;
+          if (storer) ptx::bulk_wait_read<Out::kBuffers - 1>();            // the buffer's last stores have read it
+          mx_half_sync(1 + half);
+          const uint32_t mine = to + static_cast<uint32_t>(quad * 32 + lane) * sizeof(Y);
+          if (prm.relu) mx_stage<Y, Out::kBatch, true>(mine, acc, k0, b); else mx_stage<Y, Out::kBatch, false>(mine, acc, k0, b);
+          ptx::fence_async_smem();
+          mx_half_sync(1 + half);
+          if (storer) {
+#pragma unroll
+            for (int k = 0; k < Out::kBatch; ++k)
+              if (n0 < prm.N && t0 + 32 * (k0 + k) < prm.T)
+                ptx::tma_store_2d(&map_y, to + static_cast<uint32_t>(k) * Out::kChunkBytes, n0, t0 + 32 * (k0 + k));
+            ptx::bulk_commit();                              // (also where nothing was stored: the waits count groups)
+          }
+          if (++buffer == Out::kBuffers) buffer = 0;
+        }
+      } else {
+        Y* p = y + static_cast<size_t>(t0) * prm.ld + n;
+        const int cols = n < prm.N ? prm.T - t0 : 0;
+#pragma unroll
+        for (int i = 0; i < 32 * kMxPairChunks; ++i) {
+          const float v = __uint_as_float(acc[i >> 5][i & 31]) + b;
+          if (i < cols) *p = from_float<Y>(prm.relu && v < 0.0f ? 0.0f : v);
           p += prm.ld;
         }
       }
-      ptx::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive_cluster(free0 + 8u * static_cast<uint32_t>(buf));
     }
+    if (STAGED && storer) ptx::bulk_wait_all();
   }
   // Nothing of this CTA goes away while the peer can still signal its barriers or multiply into its tensor memory.
   ptx::tc_fence_before();

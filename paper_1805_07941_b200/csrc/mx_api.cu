@@ -180,11 +180,15 @@ struct qmx_linear {
   DevicePool::Block block;
   int* d_status = nullptr;
   int device = 0, num_sms = 148;
-  CUtensorMap map_w, map_ws, map_x, map_xs;
+  CUtensorMap map_w, map_ws, map_x, map_xs, map_y;
   const uint8_t* x_codes = nullptr;      // what map_x and map_xs are of
   const uint8_t* x_scales = nullptr;
   int x_tokens = 0, x_bn = 0;
+  const void* y = nullptr;               // what map_y is of
+  int y_tokens = 0;
+  long long y_ld = 0;
   int bn = 0, split = 0, stages = 0;     // the last run's form
+  bool staged = false;
   unsigned int wait_limit = 1u << 22;
   cudaStream_t last_stream = nullptr;
 };
@@ -252,19 +256,19 @@ int launch_gemm(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   return QCONV_OK;
 }
 
-template <typename Y>
+template <typename Y, bool STAGED>
 cudaError_t allow_pair_smem() {
-  return cudaFuncSetAttribute(qc::mx_gemm_pair_kernel<Y>, cudaFuncAttributeMaxDynamicSharedMemorySize, qc::kMxPairSmem);
+  return cudaFuncSetAttribute(qc::mx_gemm_pair_kernel<Y, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (qc::kMxPairSmem<Y, STAGED>));
 }
 
-template <typename Y>
+template <typename Y, bool STAGED>
 int launch_pair(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   static qc::PerDevice<cudaError_t> allowed;
-  CUDA_TRY(allowed.once(h->device, allow_pair_smem<Y>));
+  CUDA_TRY(allowed.once(h->device, allow_pair_smem<Y, STAGED>));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2u * std::min(prm.tiles_n * prm.tiles_t, h->num_sms / 2));
   cfg.blockDim = dim3(qc::kMxPairThreads);
-  cfg.dynamicSmemBytes = qc::kMxPairSmem;
+  cfg.dynamicSmemBytes = (qc::kMxPairSmem<Y, STAGED>);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -274,9 +278,9 @@ int launch_pair(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  h->bn = qc::kMxPairTokens; h->split = 0; h->stages = qc::kMxPairStages;
-  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_pair_kernel<Y>, h->map_w, h->map_x, h->map_ws, h->map_xs, prm, h->bias, y, h->d_status,
-                              h->wait_limit));
+  h->bn = qc::kMxPairTokens; h->split = 0; h->stages = qc::kMxPairStages; h->staged = STAGED;
+  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_pair_kernel<Y, STAGED>, h->map_w, h->map_x, h->map_ws, h->map_xs, h->map_y, prm, h->bias, y,
+                              h->d_status, h->wait_limit));
   return QCONV_OK;
 }
 
@@ -349,12 +353,24 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
     if (rc) return rc;
     h->x_codes = d_x_codes; h->x_scales = d_x_scales; h->x_tokens = tokens; h->x_bn = bn;
   }
+  // (bulk stores clip at 16 bytes along a row, not at its last value)
+  const long long ysize = static_cast<long long>(type_size(d.type));
+  const bool staged = pair && aligned(d_y, 16) && ld * ysize % 16 == 0 && d.N * ysize % 16 == 0;
+  if (staged && (h->y != d_y || h->y_tokens != tokens || h->y_ld != ld)) {
+    h->y = nullptr;
+    rc = encode_2d(&h->map_y, d.type == QTYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, d_y, d.N, tokens,
+                   static_cast<cuuint64_t>(ld * ysize), 128, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+    if (rc) return rc;
+    h->y = d_y; h->y_tokens = tokens; h->y_ld = ld;
+  }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   h->last_stream = st;
   return with_type(d.type, [&](auto t) {
     using Y = decltype(t);
     Y* y = static_cast<Y*>(d_y);
-    if (pair) return launch_pair<Y>(h, prm, y, st);
+    if (pair) {
+      return staged ? launch_pair<Y, true>(h, prm, y, st) : launch_pair<Y, false>(h, prm, y, st);
+    }
     if (bn == 16) return launch_gemm<16, Y>(h, prm, y, st);
     if (bn == 32) return launch_gemm<32, Y>(h, prm, y, st);
     if (bn == 64) return launch_gemm<64, Y>(h, prm, y, st);
@@ -382,8 +398,8 @@ int qmx_linear_set_wait_limit(qmx_linear* h, unsigned int polls) {
 
 int qmx_linear_describe(const qmx_linear* h, char* buf, size_t buf_len) {
   if (!h || !buf || buf_len == 0) return fail(QCONV_ERR_BAD_ARG, "NULL argument");
-  snprintf(buf, buf_len, "mx N=%d K=%d tile=%dx%d split=%d pair=%d stages=%d", h->d.N, h->d.K, h->split == 0 ? 256 : 128, h->bn, std::max(1, h->split),
-           h->split == 0, h->stages);
+  snprintf(buf, buf_len, "mx N=%d K=%d tile=%dx%d split=%d pair=%d stages=%d staged=%d", h->d.N, h->d.K, h->split == 0 ? 256 : 128, h->bn, std::max(1, h->split),
+           h->split == 0, h->stages, h->split == 0 && h->staged);
   return QCONV_OK;
 }
 

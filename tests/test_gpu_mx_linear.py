@@ -63,12 +63,17 @@ def test_exact_sums_on_pairs_of_sms(T, N, K, dtype):
     import torch
     rng = np.random.default_rng(T + N + K)
     lin, xc, xs, _, x, w = layer(rng, T, N, K, dtype, bias=True, relu=True)
-    flat = torch.full((T * N + 64,), 77.0, dtype=lin.dtype, device="cuda")
-    y = lin.run(xc, xs, flat[:T * N].view(T, N))
-    assert lin.status() == 0 and "pair=1" in lin.describe()
     want = torch.from_numpy(x).cuda() @ torch.from_numpy(w).cuda().T + lin._keep[2].double()
-    assert torch.equal(y, want.clamp(min=0).float().to(lin.dtype))
-    assert (flat[T * N:] == 77.0).all()
+    want = want.clamp(min=0).float().to(lin.dtype)
+    for start, ld in ((0, N), (16, -(-N // 8) * 8 + 16), (1, N + 3)):       # as it comes, rows at 16 bytes, rows anywhere
+        flat = torch.full((T * ld + 64,), 77.0, dtype=lin.dtype, device="cuda")
+        y = lin.run(xc, xs, torch.as_strided(flat, (T, N), (ld, 1), start))
+        assert lin.status() == 0 and "pair=1" in lin.describe()
+        per_16_bytes = 4 if dtype == "float32" else 8
+        assert ("staged=1" in lin.describe()) == (start % per_16_bytes == 0 and ld % per_16_bytes == 0 and N % per_16_bytes == 0)
+        assert torch.equal(y, want)
+        y.fill_(77.0)
+        assert (flat == 77.0).all(), "written outside the output"
 
 
 @pytest.mark.parametrize("T,N,K", [(1, 300, 5000), (40, 200, 2000), (150, 300, 1024)])
