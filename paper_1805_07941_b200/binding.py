@@ -655,14 +655,15 @@ def qquantize_bias(b, e_x, e_w):
 # ---------------------------------------------------------------------------------------------------------------
 _types = {}
 _BYTES = ()
-_empty = None
+_INT64 = _empty = None
 
 
 def _start():
     """What the functions below look up, once."""
-    global _types, _BYTES, _empty
+    global _types, _BYTES, _INT64, _empty
     import torch
     _stream()
+    _INT64 = torch.int64
     _empty = torch.empty
     _BYTES = (torch.uint8, torch.int8)
     _types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
@@ -678,14 +679,13 @@ def _type_of(dtype):
 
 
 def _device(*tensors):
-    """The current CUDA device, which every tensor (None: not given) must be on."""
+    """Every tensor (None: not given) must be on the current CUDA device.  (Callers on the fast path ask themselves first.)"""
     if _current_device is None:
         _start()
     dev = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError("the tensors must be on the current CUDA device (%d), not on %s" % (dev, t.device))
-    return dev
 
 
 def _rows(t, what):
@@ -719,7 +719,9 @@ def qmx_quantize(x, rule=MX_COVER, layout=MX_TILES, codes=None, scales=None):
         codes = _empty((rows, pitch), dtype=_BYTES[0], device=x.device)
     if scales is None:
         scales = _empty((rows, pitch // 16) if layout == MX_ROWS else (size,), dtype=_BYTES[0], device=x.device)
-    dev = _device(x, codes, scales)
+    dev = _current_device()
+    if x.get_device() != dev or codes.get_device() != dev or scales.get_device() != dev:
+        _device(x, codes, scales)
     _bytes(codes, rows * pitch, "codes")
     _bytes(scales, size, "scales")
     if rows and K:
@@ -739,7 +741,9 @@ def qmx_dequantize(codes, scales, K, layout=MX_TILES, dtype=None, out=None):
         raise ValueError("out must be [%d, %d]" % (rows, K))
     type_ = _type_of(out.dtype)
     pitch, size = _mx_size(rows, K, layout)
-    dev = _device(codes, scales, out)
+    dev = _current_device()
+    if codes.get_device() != dev or scales.get_device() != dev or out.get_device() != dev:
+        _device(codes, scales, out)
     _bytes(codes, rows * pitch, "codes")
     _bytes(scales, size, "scales")
     if rows and K:
@@ -776,7 +780,9 @@ class QMXLinear:
         tokens = x_codes.shape[0]
         if y is None:
             y = _empty((tokens, self.N), dtype=self.dtype, device=x_codes.device)
-        dev = _device(x_codes, x_scales, y)
+        dev = _current_device()
+        if x_codes.get_device() != dev or x_scales.get_device() != dev or y.get_device() != dev:
+            _device(x_codes, x_scales, y)
         _bytes(x_codes, tokens * self._pitch, "x_codes")
         _bytes(x_scales, (tokens + 127) // 128 * self._tiles, "x_scales")
         if y.dtype != self.dtype or y.shape != (tokens, self.N):
@@ -821,30 +827,35 @@ def qrmsnorm(x, gain, eps, residual=None, sum_out=None, out=NORM_I8, e=0, layout
     (NORM_MX).  sum_out receives x + residual and may be x or residual itself."""
     dtype, shape = x.dtype, x.shape
     type_, ld, (rows, C) = _type_of(dtype), _rows(x, "x"), shape
-    ld_residual = ld_sum = residual_at = sum_at = 0
+    dev = _current_device()
+    on = x.get_device() == dev and gain.get_device() == dev
+    ld_residual = ld_sum = residual_at = sum_at = scales_at = 0
     if residual is not None:
         if residual.dtype != dtype or residual.shape != shape:
             raise ValueError("residual must be like x")
+        on = on and residual.get_device() == dev
         ld_residual, residual_at = _rows(residual, "residual"), residual.data_ptr()
     if sum_out is not None:
         if sum_out.dtype != dtype or sum_out.shape != shape:
             raise ValueError("sum_out must be like x")
+        on = on and sum_out.get_device() == dev
         ld_sum, sum_at = _rows(sum_out, "sum_out"), sum_out.data_ptr()
     if gain.dtype != dtype or gain.shape != (C,) or not gain.is_contiguous():
         raise ValueError("the gain must be %d contiguous values of x's type" % C)
     pitch, size = _mx_size(rows, C, layout) if out == NORM_MX else (C, rows)
     if codes is None:
         codes = _empty((rows, pitch), dtype=_BYTES[0 if out == NORM_MX else 1], device=x.device)
-    scales_at = 0
     if out == NORM_I8:
         scales = None
     else:
         if scales is None:
             scales = _empty((rows, pitch // 16) if out == NORM_MX and layout == MX_ROWS else (size,), dtype=_BYTES[0], device=x.device)
         _bytes(scales, size, "scales")
+        on = on and scales.get_device() == dev
         scales_at = scales.data_ptr()
-    dev = _device(x, gain, residual, sum_out, codes, scales)
     _bytes(codes, rows * pitch, "codes")
+    if not on or codes.get_device() != dev:
+        _device(x, gain, residual, sum_out, codes, scales)
     if rows and C:
         rc = (_lib or lib()).qrmsnorm(_NORM_ARGS.pack(x.data_ptr(), residual_at, gain.data_ptr(), sum_at, type_, C, rows, ld, ld_residual, ld_sum,
                                                       eps, out, e, layout, codes.data_ptr(), scales_at), _raw_stream(dev))
@@ -871,7 +882,7 @@ class QCache:
                 _bytes(c, slots * heads * (D if fmt == CACHE_I8 else blocks * 16), "codes")
                 _bytes(s, slots * heads * (1 if fmt == CACHE_I8 else blocks), "scales")
         self.slots, self.heads, self.D, self.fmt = slots, heads, D, fmt
-        self._keep = (k_codes, k_scales, v_codes, v_scales)
+        self._keep, self._alone, self._shape = (k_codes, k_scales, v_codes, v_scales), v_codes is None, (heads, D)
         self.desc = qcache_desc(int(fmt), heads, D, slots, _dev(k_codes), _dev(k_scales), _dev(v_codes), _dev(v_scales))
         self._desc = ctypes.byref(self.desc)
         self._write, self._read = lib().qcache_write, lib().qcache_read
@@ -889,18 +900,19 @@ class QCache:
 
     def _values(self, t, rows, dtype):
         strides = t.stride()
-        if t.dtype != dtype or t.shape != (rows, self.heads, self.D) or (strides[2] != 1 and self.D > 1):
-            raise ValueError("keys and values must be [%d, %d, %d] of one type with contiguous heads" % (rows, self.heads, self.D))
+        if t.dtype != dtype or t.shape != (rows,) + self._shape or (strides[2] != 1 and self.D > 1):
+            raise ValueError("keys and values must be [%d, %d, %d] of one type with contiguous heads" % ((rows,) + self._shape))
         return _CACHE_VALUES.pack(t.data_ptr(), strides[0], strides[1])
 
     def _args(self, slots, k, v):
-        if slots.dim() != 1 or not slots.is_contiguous() or slots.element_size() != 8 or slots.is_floating_point():
+        if slots.dtype != _INT64 or slots.dim() != 1 or not slots.is_contiguous():
             raise ValueError("slots must be a contiguous 1-D int64 tensor")
-        if (v is None) != (self._keep[2] is None):
+        dtype, rows, dev = k.dtype, slots.shape[0], _current_device()
+        if slots.get_device() != dev or k.get_device() != dev or (v is not None and v.get_device() != dev):
+            _device(slots, k, v)
+        if (v is None) != self._alone:
             raise ValueError("the cache holds %s" % ("keys alone" if v is not None else "keys and values"))
-        dtype, rows = k.dtype, slots.shape[0]
-        return (rows, _type_of(dtype), self._values(k, rows, dtype), None if v is None else self._values(v, rows, dtype),
-                _raw_stream(_device(slots, k, v)))
+        return (rows, _type_of(dtype), self._values(k, rows, dtype), None if v is None else self._values(v, rows, dtype), _raw_stream(dev))
 
     def write(self, slots, k, v=None):
         """Rows of k (and v) [rows, heads, D] into the slots; rows whose slot is outside the cache are skipped."""
