@@ -443,7 +443,8 @@ enum { QTYPE_F32 = 0, QTYPE_BF16 = 1, QTYPE_F16 = 2 };
  *   scales  QMX_ROWS:  [rows][ceil(K / 32)] bytes
  *           QMX_TILES: tiles of 128 rows x 4 blocks, 512 bytes each, [ceil(rows / 128)][ceil(K / 128)] of them; the byte of
  *           row r, block b is byte (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of its tile (the order the products read;
- *           16-byte aligned).  Bytes of rows and blocks that only fill up a tile are written as 127.
+ *           16-byte aligned).  Bytes of rows and blocks that only fill up a tile are written as 127; products take them
+ *           as they are: those of rows may hold anything, those of blocks anything but 255.
  * qmx_quantize: a block's scale is chosen from its largest finite magnitude,
  *   QMX_COVER  the smallest e with 6 * 2^e >= that magnitude: nothing saturates (the rule of qscale_exponent)
  *   QMX_FLOOR  e = floor(log2 of it) - 2: values above 6 * 2^e saturate (the rule of the OCP microscaling formats)
@@ -466,9 +467,9 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
  * the sum in 32 bits on the tensor cores (its order is fixed by the sizes: the same call gives the same bits), rounded once to
  * the output type.  Scales of both operands are in QMX_TILES.
  *   d_w_codes, d_w_scales   the weights, N rows of K; d_bias N float32 or NULL.  They stay the caller's, are not copied,
- *                           and must outlive the handle.
- * A handle belongs to the device that is current when it is made; running it elsewhere is BAD_ARG.  It holds no scratch:
- * runs may overlap on several streams, but one host thread uses it at a time.  Device-side waits are bounded as
+ *                           and must outlive the handle; a run reads what they hold then.
+ * A handle belongs to the device that is current when it is made (not while a stream is being captured); running it elsewhere
+ * is BAD_ARG.  It holds no scratch: runs may overlap on several streams, but one host thread uses it at a time.  Device-side waits are bounded as
  * qconv_run's are; qmx_linear_status synchronises the stream of the last run and returns (and clears) the device status,
  * qmx_linear_set_wait_limit is the test hook that qconv_set_wait_limit is. */
 typedef struct {

@@ -696,6 +696,12 @@ def _rows(t, what):
     return strides[0] if t.shape[0] > 1 else max(strides[0], t.shape[1])
 
 
+def _codes(t, rows, pitch, what):
+    """Codes that are read: contiguous, exactly rows * pitch bytes."""
+    if t.dtype not in _BYTES or t.numel() != rows * pitch or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous uint8 tensor of %d x %d bytes" % (what, rows, pitch))
+
+
 def _bytes(t, count, what):
     """A contiguous tensor of at least `count` one-byte values."""
     if t.dtype not in _BYTES or t.numel() < count or not t.is_contiguous():
@@ -744,7 +750,7 @@ def qmx_dequantize(codes, scales, K, layout=MX_TILES, dtype=None, out=None):
     dev = _current_device()
     if codes.get_device() != dev or scales.get_device() != dev or out.get_device() != dev:
         _device(codes, scales, out)
-    _bytes(codes, rows * pitch, "codes")
+    _codes(codes, rows, pitch, "codes")
     _bytes(scales, size, "scales")
     if rows and K:
         rc = (_lib or lib()).qmx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, K, layout, out.data_ptr(), type_, _rows(out, "out"),
@@ -764,7 +770,7 @@ class QMXLinear:
         self.desc = qmx_linear_desc(N=N, K=K, relu=int(relu), type=_type_of(self.dtype))
         self._pitch, size = _mx_size(N, K, MX_TILES)
         _device(w_codes, w_scales, bias)
-        _bytes(w_codes, N * self._pitch, "w_codes")
+        _codes(w_codes, N, self._pitch, "w_codes")
         _bytes(w_scales, size, "w_scales")
         if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != N):
             raise ValueError("the bias must be %d contiguous float32 values" % N)
@@ -783,7 +789,7 @@ class QMXLinear:
         dev = _current_device()
         if x_codes.get_device() != dev or x_scales.get_device() != dev or y.get_device() != dev:
             _device(x_codes, x_scales, y)
-        _bytes(x_codes, tokens * self._pitch, "x_codes")
+        _codes(x_codes, tokens, self._pitch, "x_codes")
         _bytes(x_scales, (tokens + 127) // 128 * self._tiles, "x_scales")
         if y.dtype != self.dtype or y.shape != (tokens, self.N):
             raise ValueError("y must be [%d, %d] of %s" % (tokens, self.N, self.dtype))

@@ -180,13 +180,7 @@ struct qmx_linear {
   DevicePool::Block block;
   int* d_status = nullptr;
   int device = 0, num_sms = 148;
-  CUtensorMap map_w, map_ws, map_x, map_xs, map_y;
-  const uint8_t* x_codes = nullptr;      // what map_x and map_xs are of
-  const uint8_t* x_scales = nullptr;
-  int x_tokens = 0, x_bn = 0;
-  const void* y = nullptr;               // what map_y is of
-  int y_tokens = 0;
-  long long y_ld = 0;
+  CUtensorMap map_w, map_ws;
   int bn = 0, split = 0, stages = 0;     // the last run's form
   bool staged = false;
   unsigned int wait_limit = 1u << 22;
@@ -217,13 +211,16 @@ int encode_operand(CUtensorMap* codes, CUtensorMap* scales, const uint8_t* d_cod
   return rc;
 }
 
+// The tensor maps of one run's activations, their scales and (where it is stored in bulk) its output.
+struct MxRunMaps { CUtensorMap x, xs, y; };
+
 template <int BN, typename Y>
 cudaError_t allow_gemm_smem() {
   return cudaFuncSetAttribute(qc::mx_gemm_kernel<BN, Y>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
 }
 
 template <int BN, typename Y>
-int launch_gemm(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
+int launch_gemm(qmx_linear* h, const MxRunMaps& maps, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   using Tile = qc::MxTile<BN>;
   static qc::PerDevice<cudaError_t> allowed;
   CUDA_TRY(allowed.once(h->device, allow_gemm_smem<BN, Y>));
@@ -251,7 +248,7 @@ int launch_gemm(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   cfg.attrs = attr;
   cfg.numAttrs = prm.split > 1 ? 2 : 1;
   h->bn = BN; h->split = prm.split; h->stages = prm.stages;
-  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_kernel<BN, Y>, h->map_w, h->map_x, h->map_ws, h->map_xs, prm, h->bias, y, h->d_status,
+  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_kernel<BN, Y>, h->map_w, maps.x, h->map_ws, maps.xs, prm, h->bias, y, h->d_status,
                               h->wait_limit));
   return QCONV_OK;
 }
@@ -262,7 +259,7 @@ cudaError_t allow_pair_smem() {
 }
 
 template <typename Y, bool STAGED>
-int launch_pair(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
+int launch_pair(qmx_linear* h, const MxRunMaps& maps, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   static qc::PerDevice<cudaError_t> allowed;
   CUDA_TRY(allowed.once(h->device, allow_pair_smem<Y, STAGED>));
   cudaLaunchConfig_t cfg = {};
@@ -279,7 +276,7 @@ int launch_pair(qmx_linear* h, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   h->bn = qc::kMxPairTokens; h->split = 0; h->stages = qc::kMxPairStages; h->staged = STAGED;
-  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_pair_kernel<Y, STAGED>, h->map_w, h->map_x, h->map_ws, h->map_xs, h->map_y, prm, h->bias, y,
+  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_pair_kernel<Y, STAGED>, h->map_w, maps.x, h->map_ws, maps.xs, maps.y, prm, h->bias, y,
                               h->d_status, h->wait_limit));
   return QCONV_OK;
 }
@@ -347,21 +344,16 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
   const int bn = pair ? qc::kMxPairTokens : bn_one;
   if (pair) prm.tiles_n = (d.N + 255) / 256;
   prm.tiles_t = (tokens + bn - 1) / bn;
-  if (h->x_codes != d_x_codes || h->x_scales != d_x_scales || h->x_tokens != tokens || h->x_bn != bn) {
-    h->x_codes = nullptr;
-    rc = encode_operand(&h->map_x, &h->map_xs, d_x_codes, d_x_scales, tokens, d.K, pair ? bn / 2 : bn, pair ? 256 : bn);
-    if (rc) return rc;
-    h->x_codes = d_x_codes; h->x_scales = d_x_scales; h->x_tokens = tokens; h->x_bn = bn;
-  }
+  MxRunMaps maps;
+  rc = encode_operand(&maps.x, &maps.xs, d_x_codes, d_x_scales, tokens, d.K, pair ? bn / 2 : bn, pair ? 256 : bn);
+  if (rc) return rc;
   // (bulk stores clip at 16 bytes along a row, not at its last value)
   const long long ysize = static_cast<long long>(type_size(d.type));
   const bool staged = pair && aligned(d_y, 16) && ld * ysize % 16 == 0 && d.N * ysize % 16 == 0;
-  if (staged && (h->y != d_y || h->y_tokens != tokens || h->y_ld != ld)) {
-    h->y = nullptr;
-    rc = encode_2d(&h->map_y, d.type == QTYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, d_y, d.N, tokens,
+  if (staged) {
+    rc = encode_2d(&maps.y, d.type == QTYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, d_y, d.N, tokens,
                    static_cast<cuuint64_t>(ld * ysize), 128, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
     if (rc) return rc;
-    h->y = d_y; h->y_tokens = tokens; h->y_ld = ld;
   }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   h->last_stream = st;
@@ -369,12 +361,12 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
     using Y = decltype(t);
     Y* y = static_cast<Y*>(d_y);
     if (pair) {
-      return staged ? launch_pair<Y, true>(h, prm, y, st) : launch_pair<Y, false>(h, prm, y, st);
+      return staged ? launch_pair<Y, true>(h, maps, prm, y, st) : launch_pair<Y, false>(h, maps, prm, y, st);
     }
-    if (bn == 16) return launch_gemm<16, Y>(h, prm, y, st);
-    if (bn == 32) return launch_gemm<32, Y>(h, prm, y, st);
-    if (bn == 64) return launch_gemm<64, Y>(h, prm, y, st);
-    return launch_gemm<128, Y>(h, prm, y, st);
+    if (bn == 16) return launch_gemm<16, Y>(h, maps, prm, y, st);
+    if (bn == 32) return launch_gemm<32, Y>(h, maps, prm, y, st);
+    if (bn == 64) return launch_gemm<64, Y>(h, maps, prm, y, st);
+    return launch_gemm<128, Y>(h, maps, prm, y, st);
   });
 }
 
@@ -439,7 +431,9 @@ int launch_norm(const qc::NormArgs<T>& a, int G, int warps, cudaStream_t st) {
 }
 
 // A row's values in registers: pieces of 32 bytes, one a lane for few rows (the more warps, the shorter the chain of a
-// thread), two or four for many (unaligned ones only up to two: they pass through registers one by one first).
+// thread: one row of 4096 bf16 2.5 us, 3.0 with two, 5.6 with four), two for many (16384 x 8192 bf16 into 4 bits 140 us, 189 with
+// one, 154 with four), four where a row is longer than two of every thread hold (unaligned rows only up to two: they pass
+// through registers one by one first).
 template <typename T, int OUT>
 int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
   constexpr int E = qc::Piece<T>::E;

@@ -192,6 +192,8 @@ def test_refused_tensors():
     with pytest.raises(ValueError):
         lin.run(xc, xs[:256])
     with pytest.raises(ValueError):
+        lin.run(torch.zeros((4, 48), dtype=torch.uint8, device="cuda"), xs)
+    with pytest.raises(ValueError):
         lin.run(xc.cpu(), xs)
     with pytest.raises(ValueError):
         binding.QMXLinear(xc, xs, 64, 64)
