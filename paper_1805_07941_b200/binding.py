@@ -831,21 +831,21 @@ def qrmsnorm(x, gain, eps, residual=None, sum_out=None, out=NORM_I8, e=0, layout
     """Residual addition, root-mean-square norm and conversion of x [rows, C]: (codes, scales) with int8 codes at
     exponent e (NORM_I8; scales None), int8 codes and a scale byte per row (NORM_I8_ROWS), or microscaled 4 bits
     (NORM_MX).  sum_out receives x + residual and may be x or residual itself."""
-    dtype, shape = x.dtype, x.shape
-    type_, ld, (rows, C) = _type_of(dtype), _rows(x, "x"), shape
+    dtype, strides = x.dtype, x.stride()
+    type_, ld, (rows, C) = _type_of(dtype), _rows(x, "x"), x.shape
     dev = _current_device()
     on = x.get_device() == dev and gain.get_device() == dev
     ld_residual = ld_sum = residual_at = sum_at = scales_at = 0
     if residual is not None:
-        if residual.dtype != dtype or residual.shape != shape:
+        if residual.dtype != dtype or not residual.is_same_size(x):
             raise ValueError("residual must be like x")
         on = on and residual.get_device() == dev
-        ld_residual, residual_at = _rows(residual, "residual"), residual.data_ptr()
+        ld_residual, residual_at = ld if residual.stride() == strides else _rows(residual, "residual"), residual.data_ptr()
     if sum_out is not None:
-        if sum_out.dtype != dtype or sum_out.shape != shape:
+        if sum_out.dtype != dtype or not sum_out.is_same_size(x):
             raise ValueError("sum_out must be like x")
         on = on and sum_out.get_device() == dev
-        ld_sum, sum_at = _rows(sum_out, "sum_out"), sum_out.data_ptr()
+        ld_sum, sum_at = ld if sum_out.stride() == strides else _rows(sum_out, "sum_out"), sum_out.data_ptr()
     if gain.dtype != dtype or gain.shape != (C,) or not gain.is_contiguous():
         raise ValueError("the gain must be %d contiguous values of x's type" % C)
     pitch, size = _mx_size(rows, C, layout) if out == NORM_MX else (C, rows)

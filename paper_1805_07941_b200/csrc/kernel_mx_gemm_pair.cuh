@@ -69,9 +69,8 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
                ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1) : "memory");
 }
-// All but the N most recent groups of this thread's bulk stores have read their source; all of them are complete.
+// All but the N most recent groups of this thread's bulk stores have read their source.
 template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void sts_u16(uint32_t addr, uint32_t v) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(static_cast<unsigned short>(v)) : "memory");
 }
@@ -352,7 +351,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         }
       }
     }
-    if (STAGED && storer) ptx::bulk_wait_all();
+    if (STAGED && storer) ptx::bulk_wait_read<0>();           // shared memory stays until it has been read (the grid's end waits for the writes)
   }
   // Nothing of this CTA goes away while the peer can still signal its barriers or multiply into its tensor memory.
   ptx::tc_fence_before();
