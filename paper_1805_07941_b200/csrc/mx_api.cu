@@ -226,11 +226,11 @@ int launch_gemm(qmx_linear* h, const MxRunMaps& maps, qc::MxGemmParams prm, Y* y
   CUDA_TRY(allowed.once(h->device, allow_gemm_smem<BN, Y>));
   const int per_cta = (prm.k_stages + prm.split - 1) / prm.split;
   // Two CTAs an SM, so that one drains (or sets up, in the next launch) while the other multiplies; a deeper ring instead where
-  // every CTA has an SM to itself and walks a long part of the contraction on wide stages (us with half an SM's memory / all of
-  // it: 48 tokens x 16384 x 8192 17.3 / 16.0, 128 x 8192 x 8192 16.5 / 13.6; the other way round 64 x 4096 x 4096, four stages
-  // a CTA, 5.3 / 6.0).  A shared tile's sums have shared memory of their own.
+  // every CTA has an SM to itself and walks a long part of the contraction (us with half an SM's memory / all of it: 48 tokens x
+  // 16384 x 8192 17.3 / 16.0, 128 x 8192 x 8192 16.5 / 13.6, 1 x 8192 x 28672 22.7 / 22.3; the other way round 64 x 4096 x 4096,
+  // four stages a CTA, 5.3 / 6.0).  A shared tile's sums have shared memory of their own.
   const uint32_t sums = prm.split > 1 ? 16 + std::max(BN, 4 * prm.split) * 512 : 0;
-  const bool alone = prm.tiles_n * prm.tiles_t * prm.split <= h->num_sms && BN >= 64 && per_cta >= 8;
+  const bool alone = prm.tiles_n * prm.tiles_t * prm.split <= h->num_sms && per_cta >= 8;
   const uint32_t room = (alone ? 227u : 113u) * 1024 - 1024 - sizeof(qc::MxGemmShared) - sums;
   prm.stages = std::max(2, std::min({per_cta, static_cast<int>(room / Tile::kStage), Tile::kMaxStages}));
   const size_t smem = 1024 + static_cast<size_t>(prm.stages) * Tile::kStage + sizeof(qc::MxGemmShared) + sums;

@@ -60,6 +60,19 @@ __device__ __forceinline__ float2 unpack_two(uint32_t w, __half) {
 
 constexpr uint32_t kInfBits = 0x7F800000u;
 
+// max(m, |a|, |b|) in one instruction; NaN if any of them is.
+__device__ __forceinline__ float max_abs(float m, float a, float b) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(a), "f"(b));
+  return r;
+}
+// The larger of each two 16-bit numbers.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // How a row of values may be reached.
 enum : int { ROWS_ANY = 0, ROWS_16 = 1, ROWS_32 = 2 };     // one value at a time; in 16-byte pieces; in 32-byte pieces
 
@@ -112,20 +125,20 @@ template <typename T> struct Piece {
       for (int i = 0; i < 8; ++i) w[i] = pack_two(v[2 * i], v[2 * i + 1], T());
     }
   }
-  // Bits, as float32's, of the largest magnitude (magnitudes order like their bit patterns, NaN above infinity): for 16-bit
-  // types two at a time.
+  // Bits, as float32's, of the largest magnitude, at least infinity's if one is not finite; for 16-bit types two at a time
+  // (magnitudes order like their bit patterns, NaN above infinity).
   __device__ __forceinline__ uint32_t top() const {
     if constexpr (sizeof(T) == 4) {
-      uint32_t m = 0;
+      float m = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
-      return m;
+      for (int i = 0; i < 8; i += 2) m = max_abs(m, __uint_as_float(w[i]), __uint_as_float(w[i + 1]));
+      return __float_as_uint(m);
     } else {
       uint32_t m = w[0] & 0x7FFF7FFFu;
 #pragma unroll
-      for (int i = 1; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+      for (int i = 1; i < 8; ++i) m = max_u16x2(m, w[i] & 0x7FFF7FFFu);
       m = max(m & 0xFFFFu, m >> 16);
-      if constexpr (sizeof(T) == 2 && static_cast<bool>(__is_same(T, __half)))
+      if constexpr (static_cast<bool>(__is_same(T, __half)))
         return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(m))));
       else
         return m << 16;
@@ -205,13 +218,14 @@ __device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int 
   }
 }
 
-// Bits of the largest |v| over a lane's values; over the finite ones alone, with NaN made 0 in v (infinities stay: they saturate).
+// Bits of the largest |v| over a lane's values, at least infinity's if one is not finite; over the finite ones alone, with
+// NaN made 0 in v (infinities stay: they saturate).
 template <int E>
 __device__ __forceinline__ uint32_t top_bits(const float (&v)[E]) {
-  uint32_t m = 0;
+  float m = 0.0f;
 #pragma unroll
-  for (int i = 0; i < E; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  return m;
+  for (int i = 0; i < E; i += 2) m = max_abs(m, v[i], v[i + 1]);
+  return __float_as_uint(m);
 }
 template <int E>
 __device__ __forceinline__ uint32_t top_bits_finite(float (&v)[E]) {
