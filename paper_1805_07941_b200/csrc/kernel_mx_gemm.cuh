@@ -116,6 +116,32 @@ template <int BN> struct MxTile {
   static_assert(BN <= 128 && kMaxStages >= 2 && kStage % 1024 == 0);
 };
 
+// Stores a lane's sums of COUNT consecutive tokens (one channel, rows `ld` apart; the first `cols` count): bias, ReLU and
+// rounding first, in place, then one store after the other from eight pointers.  A store reads its registers some tens of
+// cycles after it was issued; with one value and one pointer that are made anew for each, a warp stores every 40 to 50 cycles.
+template <int COUNT, typename Y>
+__device__ __forceinline__ void mx_store_column(uint32_t (&acc)[COUNT], Y* y, size_t ld, int cols, float bias, bool relu) {
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) {
+    float v = __uint_as_float(acc[i]) + bias;
+    if (relu) v = v < 0.0f ? 0.0f : v;
+    const Y r = from_float<Y>(v);
+    if constexpr (sizeof(Y) == 4) acc[i] = __float_as_uint(v);
+    else acc[i] = *reinterpret_cast<const unsigned short*>(&r);
+  }
+  Y* p[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p[i] = y + i * ld;
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) {
+    if (i < cols) {
+      if constexpr (sizeof(Y) == 4) *reinterpret_cast<uint32_t*>(p[i & 7]) = acc[i];
+      else *reinterpret_cast<unsigned short*>(p[i & 7]) = static_cast<unsigned short>(acc[i]);
+    }
+    p[i & 7] += 8 * ld;
+  }
+}
+
 // Columns that a warp drains at a time.
 template <int BN> constexpr int kMxChunk = BN < 32 ? 16 : 32;
 template <int BN>
@@ -151,12 +177,13 @@ __device__ __forceinline__ void mx_exchange(uint32_t lane_addr, uint32_t exchang
       const float4 w = ptx::lds_float4(mine + static_cast<uint32_t>(g / SPLIT * SPLIT + p) * kPlace);
       v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
     }
-    done(4 * g, v);
+    uint32_t bits[4] = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    done(4 * g, bits);
   }
 }
 
 template <int BN, typename Y>
-__global__ void __launch_bounds__(kMxGemmThreads)
+__global__ void __launch_bounds__(kMxGemmThreads, 2)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const MxGemmParams prm,
                const float* __restrict__ bias, Y* __restrict__ y, int* status, unsigned int wait_limit) {
@@ -286,24 +313,17 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   const int n = n0 + static_cast<int>(threadIdx.x);
   const uint32_t lane_addr = tmem + (static_cast<uint32_t>(warp * 32) << 16);
   const float b = bias != nullptr && n < prm.N ? __ldg(bias + n) : 0.0f;
-  auto store = [&](int t, float v) {
-    v += b;
-    if (prm.relu) v = v < 0.0f ? 0.0f : v;
-    if (t < prm.T && n < prm.N) y[static_cast<size_t>(t) * prm.ld + n] = from_float<Y>(v);
-  };
   if (split == 1) {
     if (good)
       for (int c = 0; c < BN && t0 + c < prm.T; c += kMxChunk<BN>) {
         uint32_t acc[kMxChunk<BN>];
         mx_drain<BN>(lane_addr + c, acc);
-#pragma unroll
-        for (int i = 0; i < kMxChunk<BN>; ++i) store(t0 + c + i, __uint_as_float(acc[i]));
+        mx_store_column(acc, y + static_cast<size_t>(t0 + c) * prm.ld + n, prm.ld, n < prm.N ? prm.T - t0 - c : 0, b, prm.relu);
       }
   } else {
     ptx::cluster_wait();                                     // (the other CTAs run)
-    auto sums = [&](int c, float (&v)[4]) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) store(t0 + c + i, v[i]);
+    auto sums = [&](int c, uint32_t (&v)[4]) {
+      mx_store_column(v, y + static_cast<size_t>(t0 + c) * prm.ld + n, prm.ld, n < prm.N ? prm.T - t0 - c : 0, b, prm.relu);
     };
     const int cols = good ? min(BN, prm.T - t0) : 0;
     if (split == 2) mx_exchange<2, BN>(lane_addr, exchange_addr, part, cols, sums);

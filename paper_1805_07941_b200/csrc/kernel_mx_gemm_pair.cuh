@@ -341,14 +341,9 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
           if (++buffer == Out::kBuffers) buffer = 0;
         }
       } else {
-        Y* p = y + static_cast<size_t>(t0) * prm.ld + n;
-        const int cols = n < prm.N ? prm.T - t0 : 0;
 #pragma unroll
-        for (int i = 0; i < 32 * kMxPairChunks; ++i) {
-          const float v = __uint_as_float(acc[i >> 5][i & 31]) + b;
-          if (i < cols) *p = from_float<Y>(prm.relu && v < 0.0f ? 0.0f : v);
-          p += prm.ld;
-        }
+        for (int k = 0; k < kMxPairChunks; ++k)
+          mx_store_column(acc[k], y + static_cast<size_t>(t0 + 32 * k) * prm.ld + n, prm.ld, n < prm.N ? prm.T - t0 - 32 * k : 0, b, prm.relu);
       }
     }
     if (STAGED && storer) ptx::bulk_wait_read<0>();           // shared memory stays until it has been read (the grid's end waits for the writes)

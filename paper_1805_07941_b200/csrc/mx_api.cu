@@ -332,15 +332,22 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
   const long long tiles_one = static_cast<long long>((d.N + 127) / 128) * ((tokens + bn_one - 1) / bn_one);
   const long long tiles_pair = static_cast<long long>((d.N + 255) / 256) * ((tokens + qc::kMxPairTokens - 1) / qc::kMxPairTokens);
   if (tiles_one > (1ll << 27)) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "product too large");
-  prm.split = 1;
-  while (prm.split < 8 && tiles_one * prm.split * 2 <= h->num_sms && prm.split * 2 <= prm.k_stages) prm.split *= 2;
-  // Tiles on pairs of SMs take about 0.36 us a stage and wave, those of single SMs 0.5 us, and sharing a tile 2 us more (us,
-  // single / pair: 128 tokens x 8192 x 8192 13.6 / 14.6, 256 x 4096 x 4096 9.2 / 8.4, 512 x 4096 x 4096 11.8 / 9.0, 256 x 8192 x
-  // 8192 20.1 / 14.9, 1024 x 2048 x 4096 10.8 / 8.7); up to 64 tokens a pair's columns are mostly empty.
-  const int wave_pair = h->num_sms / 2;
-  const double us_pair = 0.36 * prm.k_stages * ((tiles_pair + wave_pair - 1) / wave_pair);
-  const double us_one = 0.5 * ((prm.k_stages + prm.split - 1) / prm.split) * ((tiles_one * prm.split + h->num_sms - 1) / h->num_sms) + (prm.split > 1 ? 2.0 : 0.0);
-  const bool pair = tokens > 64 && us_pair <= us_one;
+  // The form with the shortest estimate, in us without the launch.  Tiles on single SMs: 0.25 a stage and 0.35 for the output of
+  // each round of tiles, two CTAs of an SM taking turns; sharing a tile 0.018 a column more.  On pairs: 0.33 a stage and round.  (us,
+  // single / pair: 128 x 128 x 128 3.4 / 3.9, 700 x 700 x 700 4.2 / 4.8, 2048 x 2048 x 2048 7.8 / 9.1, 1024 x 4096 x 4096 11.5 / 13.8,
+  // 384 x 8192 x 8192 18.2 / 15.0, 5555 x 422 x 152 6.1 / 5.3; shared by 1 / 2 / 4 / 8: 1 x 4096 x 4096 5.7 / 4.4 / 3.6 / 4.4,
+  // 300 x 300 x 8192 10.7 / 8.7 / 6.7 / 6.3.)  More than two tiles an SM are pairs' (1000 x 5000 x 2000 17.1 / 11.5), but up to
+  // 64 tokens a pair's columns are mostly empty.  Clusters of eight: sixteen of them with more than half an SM's memory a CTA do
+  // not run at once (2025 x 64 x 2880 11.0, shared by four 5.8).
+  const auto rounds = [&](long long tiles, int at_once) { return static_cast<double>((tiles + at_once - 1) / at_once); };
+  double us_one = 0.0;
+  for (int split = 1; split <= 8 && split <= prm.k_stages; split *= 2) {
+    if (split > 1 && tiles_one * split > (split == 8 ? h->num_sms * 2 / 3 : h->num_sms)) break;
+    const double us = (0.25 * ((prm.k_stages + split - 1) / split) + 0.35) * rounds(tiles_one * split, h->num_sms) + (split > 1 ? 0.018 * bn_one : 0.0);
+    if (split == 1 || us < us_one) { us_one = us; prm.split = split; }
+  }
+  const double us_pair = 0.6 + 0.33 * prm.k_stages * rounds(tiles_pair, h->num_sms / 2);
+  const bool pair = tokens > 64 && (tiles_one > 2 * h->num_sms || us_pair < us_one);
   const int bn = pair ? qc::kMxPairTokens : bn_one;
   if (pair) prm.tiles_n = (d.N + 255) / 256;
   prm.tiles_t = (tokens + bn - 1) / bn;
