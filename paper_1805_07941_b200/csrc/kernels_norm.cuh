@@ -7,7 +7,9 @@
 // are whole numbers, and a last-bit difference in r would move those that lie next to a border.
 //
 // Bound by HBM: x, residual and h once, the codes once.  A row's values stay in registers from the load to the
-// conversion: V pieces of 32 bytes a thread, and as many lanes or warps as that makes for the row's length.
+// conversion: V pieces of 32 bytes a thread, and as many lanes or warps as that makes for the row's length.  16384 x 8192 bf16
+// with a residual into 4 bits: 139 us, 0.98 of the measured copy rate (73 % of the issue slots); rows whose pieces are not
+// aligned pass through shared memory (3000 x 1155 float32 13.7 us, 3000 x 1152 11.6).
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
