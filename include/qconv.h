@@ -469,7 +469,8 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
  *   d_w_codes, d_w_scales   the weights, N rows of K; d_bias N float32 or NULL.  They stay the caller's, are not copied,
  *                           and must outlive the handle; a run reads what they hold then.
  * A handle belongs to the device that is current when it is made (not while a stream is being captured); running it elsewhere
- * is BAD_ARG.  It holds no scratch: runs may overlap on several streams, but one host thread uses it at a time.  Device-side waits are bounded as
+ * is BAD_ARG.  It holds no scratch: runs may overlap on several streams, but one host thread uses it at a time.  Dropping it
+ * waits for the device.  Device-side waits are bounded as
  * qconv_run's are; qmx_linear_status synchronises the stream of the last run and returns (and clears) the device status,
  * qmx_linear_set_wait_limit is the test hook that qconv_set_wait_limit is. */
 typedef struct {

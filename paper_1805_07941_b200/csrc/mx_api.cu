@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <mutex>
 #include <new>
 
 #include "../../include/qconv.h"
@@ -172,19 +173,62 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
 // --------------------------------------------------------------------------- products
 }  // extern "C"
 
+// The handles' status words: up to 1024 a device out of one allocation that stays (4 KB), so that making and dropping a handle
+// costs no cudaMalloc and cudaFree (13 us instead of 0.8 ms where it is the device's only one); more come from the pool.
+class StatusWords {
+ public:
+  static StatusWords& words() {
+    static StatusWords* w = new StatusWords;               // never destroyed, as the pool
+    return *w;
+  }
+  cudaError_t take(int device, int** word) {
+    std::lock_guard<std::mutex> lock(mu_);
+    PerDevice& d = per_device_[device & 63];
+    if (!d.base) {
+      const cudaError_t e = DevicePool::pool().plain(&d.base, kWords * sizeof(int));
+      if (e != cudaSuccess) { d.base = nullptr; return e; }
+    }
+    *word = nullptr;
+    for (int i = 0; i < kWords && !*word; ++i)
+      if (!d.used[i]) { d.used[i] = true; *word = d.base + i; }
+    return cudaSuccess;
+  }
+  void give(int device, int* word) {
+    std::lock_guard<std::mutex> lock(mu_);
+    PerDevice& d = per_device_[device & 63];
+    d.used[word - d.base] = false;
+  }
+
+ private:
+  static constexpr int kWords = 1024;
+  struct PerDevice {
+    int* base = nullptr;
+    bool used[kWords] = {};
+  };
+  std::mutex mu_;
+  PerDevice per_device_[64];
+};
+
 struct qmx_linear {
   qmx_linear_desc d;
-  const uint8_t* w_codes;
-  const uint8_t* w_scales;
   const float* bias;
-  DevicePool::Block block;
+  DevicePool::Block block;               // of the status word where StatusWords has none left
   int* d_status = nullptr;
   int device = 0, num_sms = 148;
   CUtensorMap map_w, map_ws;
   int bn = 0, split = 0, stages = 0;     // the last run's form
-  bool staged = false;
+  bool pair = false, staged = false;
   unsigned int wait_limit = 1u << 22;
   cudaStream_t last_stream = nullptr;
+  ~qmx_linear() {
+    if (!d_status || block.ptr) return;
+    // (whoever takes the word next must not see a status of this handle's)
+    int dev = 0;
+    const bool other = cudaGetDevice(&dev) == cudaSuccess && dev != device && cudaSetDevice(device) == cudaSuccess;
+    cudaDeviceSynchronize();
+    if (other) cudaSetDevice(dev);
+    StatusWords::words().give(device, d_status);
+  }
 };
 
 namespace {
@@ -247,7 +291,7 @@ int launch_gemm(qmx_linear* h, const MxRunMaps& maps, qc::MxGemmParams prm, Y* y
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = prm.split > 1 ? 2 : 1;
-  h->bn = BN; h->split = prm.split; h->stages = prm.stages;
+  h->bn = BN; h->split = prm.split; h->stages = prm.stages; h->pair = h->staged = false;
   CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_kernel<BN, Y>, h->map_w, maps.x, h->map_ws, maps.xs, prm, h->bias, y, h->d_status,
                               h->wait_limit));
   return QCONV_OK;
@@ -275,7 +319,7 @@ int launch_pair(qmx_linear* h, const MxRunMaps& maps, qc::MxGemmParams prm, Y* y
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  h->bn = qc::kMxPairTokens; h->split = 0; h->stages = qc::kMxPairStages; h->staged = STAGED;
+  h->bn = qc::kMxPairTokens; h->split = 1; h->stages = qc::kMxPairStages; h->pair = true; h->staged = STAGED;
   CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_pair_kernel<Y, STAGED>, h->map_w, maps.x, h->map_ws, maps.xs, maps.y, prm, h->bias, y,
                               h->d_status, h->wait_limit));
   return QCONV_OK;
@@ -297,13 +341,16 @@ int qmx_linear_create(qmx_linear** out, const qmx_linear_desc* desc, const uint8
   qmx_linear* h = new (std::nothrow) qmx_linear();
   if (!h) return fail(QCONV_ERR_CUDA, "qmx_linear_create: out of host memory");
   h->d = *desc;
-  h->w_codes = d_w_codes; h->w_scales = d_w_scales; h->bias = d_bias;
+  h->bias = d_bias;
   rc = encode_operand(&h->map_w, &h->map_ws, d_w_codes, d_w_scales, desc->N, desc->K, 128, 128);
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
-  if (!rc && e == cudaSuccess) e = DevicePool::pool().take(&h->block, sizeof(int));
-  if (!rc && e == cudaSuccess) {
+  if (!rc && e == cudaSuccess) e = StatusWords::words().take(h->device, &h->d_status);
+  if (!rc && e == cudaSuccess && !h->d_status) {
+    e = DevicePool::pool().take(&h->block, sizeof(int));
     h->d_status = static_cast<int*>(h->block.ptr);
+  }
+  if (!rc && e == cudaSuccess) {
     const int zero = 0;
     e = cudaMemcpy(h->d_status, &zero, sizeof(int), cudaMemcpyHostToDevice);
   }
@@ -397,8 +444,8 @@ int qmx_linear_set_wait_limit(qmx_linear* h, unsigned int polls) {
 
 int qmx_linear_describe(const qmx_linear* h, char* buf, size_t buf_len) {
   if (!h || !buf || buf_len == 0) return fail(QCONV_ERR_BAD_ARG, "NULL argument");
-  snprintf(buf, buf_len, "mx N=%d K=%d tile=%dx%d split=%d pair=%d stages=%d staged=%d", h->d.N, h->d.K, h->split == 0 ? 256 : 128, h->bn, std::max(1, h->split),
-           h->split == 0, h->stages, h->split == 0 && h->staged);
+  snprintf(buf, buf_len, "mx N=%d K=%d tile=%dx%d split=%d pair=%d stages=%d staged=%d", h->d.N, h->d.K, h->pair ? 256 : 128, h->bn, h->split,
+           h->pair, h->stages, h->staged);
   return QCONV_OK;
 }
 

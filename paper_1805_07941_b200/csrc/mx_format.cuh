@@ -23,9 +23,6 @@ constexpr int kMxTileRows = 128, kMxTileBlocks = 4, kMxTileBytes = 512;
 constexpr uint32_t kScaleOne = 127u;            // the byte of 2^0; also that of a block without a finite value but zero
 
 enum : int { TYPE_F32 = 0, TYPE_BF16 = 1, TYPE_F16 = 2 };
-template <int TYPE> struct TypeOf { using type = float; };
-template <> struct TypeOf<TYPE_BF16> { using type = __nv_bfloat16; };
-template <> struct TypeOf<TYPE_F16> { using type = __half; };
 
 __host__ __device__ __forceinline__ int mx_blocks(int k) { return (k + kMxBlock - 1) / kMxBlock; }
 __host__ __device__ __forceinline__ int mx_tiles_k(int k) { return (mx_blocks(k) + kMxTileBlocks - 1) / kMxTileBlocks; }
