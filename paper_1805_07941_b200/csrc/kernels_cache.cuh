@@ -3,7 +3,7 @@
 // HBM on long lists and by the launch on short ones: keys and values go in one launch, a head takes LANES lanes with V
 // pieces of 32 bytes each, and a group of lanes has kCacheUnroll heads in flight and the slots of the next ones on their
 // way (slot, then codes and scales, are dependent loads).  131072 tokens x 8 heads x 128 bf16, keys and values, int8: written in
-// 146 us (0.85 of the measured copy rate), read back in 135 (0.93); heads of 80 values fill five of eight lanes (0.63).
+// 146 us (0.85 of the measured copy rate), read back in 135 (0.93).
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
@@ -28,7 +28,9 @@ struct CacheArgs {
   int items;                 // rows * sides * heads, below 2^30
   FastDiv fd_heads;
   int sides;
-  int how, code_vec;         // ROWS_* of the values; a lane's int8 codes are aligned
+  int unit;                  // bytes that heads of values may be reached in
+  int lanes;                 // of a head, to be written
+  int code_vec;              // a lane's int8 codes are aligned
   int code_pitch, scale_pitch;   // bytes of a head's codes and scales
 };
 
@@ -65,23 +67,50 @@ __device__ __forceinline__ T* cache_values(const CacheArgs& a, const CacheItem& 
   return static_cast<T*>(c.second ? a.side[1].values : a.side[0].values) + c.values;
 }
 
-// LANES lanes a head, V pieces a lane.
+// How the lanes of a warp share out heads.  FEW: as few each as hold one, above LANES / 2, and the lanes behind the last
+// whole group are idle.  Else LANES each.  (32768 tokens x 8 heads of bf16 to int8, few: 80 values 29.1 us, 96 34.1, 128
+// 38.5; whole: 39.0, 39.4, 39.4.  Back, few: 30.5, 35.6, 40.9; whole: 32.5, 33.9, 36.4, so that reading has it whole.)
+template <int LANES, bool FEW> struct CacheLanes {
+  int G, per_warp, lane, mine;   // mine: which of the warp's heads, past all items where idle
+  __device__ __forceinline__ CacheLanes(const CacheArgs& a) {
+    const int l = threadIdx.x & 31;
+    G = FEW ? a.lanes : LANES;
+    per_warp = 32 / G;
+    mine = l / G;
+    lane = l - mine * G;
+    if (FEW && mine >= per_warp) mine = a.items;
+  }
+  // Maximum over a head's lanes: each looks 1, 2, 4, ... lanes ahead, around the group's end.
+  __device__ __forceinline__ uint32_t max_over_head(uint32_t m) const {
+    if constexpr (!FEW) {
+      return max_over<LANES>(m);
+    } else {
+      const int first = (threadIdx.x & 31) - lane;
+#pragma unroll
+      for (int d = 1; d < LANES; d *= 2) m = max(m, __shfl_sync(0xffffffffu, m, first + (lane + d < G ? lane + d : lane + d - G)));
+      return m;
+    }
+  }
+};
+
+// Up to LANES lanes a head, V pieces a lane.  ANY: values or int8 codes that a lane cannot reach by itself go through shared
+// memory, in a part for LANES lanes.
 template <typename T, int FMT, int LANES, int V, bool ANY>
 __global__ void __launch_bounds__(kCacheThreads, V == 1 ? kCacheBlocks : 1)
 cache_write_kernel(const CacheArgs a) {
-  constexpr int E = Piece<T>::E, U = V == 1 ? kCacheUnroll : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
-  __shared__ uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
+  constexpr int E = Piece<T>::E, U = V == 1 ? kCacheUnroll : 1;
+  __shared__ __align__(16) uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int lane = threadIdx.x & (LANES - 1);
-  const int step = gridDim.x * kPerBlock;
+  const CacheLanes<LANES, !ANY> at(a);
+  const int lane = at.lane, G = at.G, mine = at.mine, per_block = kCacheThreads / 32 * at.per_warp, step = gridDim.x * per_block;
   uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
   // the lanes of a warp run the same number of rounds
-  const int warp_first = (threadIdx.x >> 5) * kPerWarp, mine = (threadIdx.x & 31) / LANES;
+  const int warp_first = (threadIdx.x >> 5) * at.per_warp;
   long long slot[U];
 #pragma unroll
-  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, blockIdx.x * kPerBlock + warp_first + j * step + mine);
-  for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += U * step) {
+  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, blockIdx.x * per_block + warp_first + j * step + mine);
+  for (int base = blockIdx.x * per_block + warp_first; base < a.items; base += U * step) {
     CacheItem c[U];
     Piece<T> x[U][V];
 #pragma unroll
@@ -92,7 +121,7 @@ cache_write_kernel(const CacheArgs a) {
     for (int j = 0; j < U; ++j)
 #pragma unroll
       for (int k = 0; k < V; ++k)
-        group_load<ANY>(x[j][k], cache_values<T>(a, c[j]) + k * LANES * E, c[j].valid ? a.D - k * LANES * E : 0, LANES, lane, a.how, stage);
+        group_load<ANY>(x[j][k], cache_values<T>(a, c[j]) + k * G * E, c[j].valid ? a.D - k * G * E : 0, G, lane, a.unit, stage);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       uint8_t* codes = cache_codes(a, c[j]);
@@ -105,30 +134,32 @@ cache_write_kernel(const CacheArgs a) {
           x[j][k].unpack(v[k]);
           m = max(m, finite_top<1>(v[k], x[j][k].top()));
         }
-        const uint32_t sb = i8_scale_byte(max_over<LANES>(m));
+        const uint32_t sb = i8_scale_byte(at.max_over_head(m));
         const float inv = inverse_scale(sb);
         if (c[j].valid && lane == 0) *scales = static_cast<uint8_t>(sb);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const int col = (k * LANES + lane) * E, n = min(E, a.D - col);
+          const int first = k * G * E, n = c[j].valid ? min(a.D - first, G * E) : 0;
           uint32_t w[E / 4];
 #pragma unroll
           for (int i = 0; i < E / 4; ++i) w[i] = i8_encode_four(v[k] + 4 * i, inv);
-          if (!c[j].valid || n <= 0) continue;
-          if (a.code_vec) {
-            if constexpr (E == 8) *reinterpret_cast<uint2*>(codes + col) = make_uint2(w[0], w[1]);
-            else *reinterpret_cast<uint4*>(codes + col) = make_uint4(w[0], w[1], w[2], w[3]);
-          } else {
+          if constexpr (ANY) {
+            uint8_t* group = stage + ((threadIdx.x & 31) - lane) * E;
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-              if (i < n) codes[col + i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i & 3)));
+            for (int i = 0; i < E / 4; ++i) reinterpret_cast<uint32_t*>(group)[lane * (E / 4) + i] = w[i];
+            __syncwarp();
+            store_bytes<E>(codes + first, group, n, G, lane);
+            __syncwarp();
+          } else if (lane * E < n) {
+            if constexpr (E == 8) *reinterpret_cast<uint2*>(codes + first + lane * E) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint4*>(codes + first + lane * E) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
       } else {
         constexpr int kBlockLanes = kMxBlock / E;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const int col = (k * LANES + lane) * E;
+          const int col = (k * G + lane) * E;
           float v[E];
           x[j][k].unpack(v);
           const uint32_t sb = mx_scale_byte(finite_top<kBlockLanes>(v, x[j][k].top()), kCoverRoundUp);
@@ -144,10 +175,11 @@ cache_write_kernel(const CacheArgs a) {
 template <typename T, int FMT, int LANES, int V, bool ANY>
 __global__ void __launch_bounds__(kCacheThreads, V == 1 ? kCacheBlocks : 1)
 cache_read_kernel(const CacheArgs a) {
-  constexpr int E = Piece<T>::E, U = V == 1 ? kCacheUnroll : 1, kPerBlock = kCacheThreads / LANES, kPerWarp = 32 / LANES;
-  __shared__ uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
+  constexpr int E = Piece<T>::E, U = V == 1 ? kCacheUnroll : 1;
+  __shared__ __align__(16) uint8_t stages[ANY ? kCacheThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
+  constexpr int kPerWarp = 32 / LANES, kPerBlock = kCacheThreads / LANES;
   const int lane = threadIdx.x & (LANES - 1);
   const int step = gridDim.x * kPerBlock;
   uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
@@ -158,6 +190,7 @@ cache_read_kernel(const CacheArgs a) {
   for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += U * step) {
     CacheItem c[U];
     uint32_t w[U][V][E / 4], sb[U][V];                      // (4-bit codes: the first half)
+    DealtBytes<E> raw[FMT == CACHE_I8 && ANY ? U : 1][V];
 #pragma unroll
     for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine, slot[j]);
 #pragma unroll
@@ -172,21 +205,25 @@ cache_read_kernel(const CacheArgs a) {
 #pragma unroll
         for (int i = 0; i < E / 4; ++i) w[j][k][i] = 0u;
         sb[j][k] = kScaleOne;
+        if constexpr (FMT == CACHE_I8 && ANY)
+          load_bytes<E>(raw[j][k], codes + k * LANES * E, c[j].valid ? min(a.D - k * LANES * E, LANES * E) : 0, LANES, lane);
         if (n <= 0) continue;
         if constexpr (FMT == CACHE_I8) {
           sb[j][k] = __ldg(scales);
-          if (a.code_vec) {
-            if constexpr (E == 8) {
-              const uint2 q = __ldg(reinterpret_cast<const uint2*>(codes + col));
-              w[j][k][0] = q.x; w[j][k][1] = q.y;
+          if constexpr (!ANY) {
+            if (a.code_vec) {
+              if constexpr (E == 8) {
+                const uint2 q = __ldg(reinterpret_cast<const uint2*>(codes + col));
+                w[j][k][0] = q.x; w[j][k][1] = q.y;
+              } else {
+                const uint4 q = __ldg(reinterpret_cast<const uint4*>(codes + col));
+                w[j][k][0] = q.x; w[j][k][1] = q.y; w[j][k][2] = q.z; w[j][k][3] = q.w;
+              }
             } else {
-              const uint4 q = __ldg(reinterpret_cast<const uint4*>(codes + col));
-              w[j][k][0] = q.x; w[j][k][1] = q.y; w[j][k][2] = q.z; w[j][k][3] = q.w;
-            }
-          } else {
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-              if (i < n) w[j][k][i / 4] |= static_cast<uint32_t>(__ldg(codes + col + i)) << (8 * (i & 3));
+              for (int i = 0; i < E; ++i)
+                if (i < n) w[j][k][i / 4] |= static_cast<uint32_t>(__ldg(codes + col + i)) << (8 * (i & 3));
+            }
           }
         } else {
           sb[j][k] = __ldg(scales + col / kMxBlock);
@@ -206,6 +243,9 @@ cache_read_kernel(const CacheArgs a) {
       for (int k = 0; k < V; ++k) {
         float v[E];
         const float scale = scale_of(sb[j][k]);
+        if constexpr (FMT == CACHE_I8 && ANY)
+          gather_bytes<E>(w[j][k], raw[j][k], cache_codes(a, c[j]) + k * LANES * E, c[j].valid ? min(a.D - k * LANES * E, LANES * E) : 0, LANES, lane,
+                          stage + (threadIdx.x & 31) / LANES * kStagedBytes<E, LANES>);
         if constexpr (FMT == CACHE_I8) {
 #pragma unroll
           for (int i = 0; i < E / 4; ++i) i8_decode_four(w[j][k][i], scale, v + 4 * i);
@@ -215,7 +255,7 @@ cache_read_kernel(const CacheArgs a) {
         }
         Piece<T> p;
         p.pack(v);
-        group_store<ANY>(p, y + k * LANES * E, c[j].valid ? a.D - k * LANES * E : 0, LANES, lane, a.how, stage);
+        group_store<ANY>(p, y + k * LANES * E, c[j].valid ? a.D - k * LANES * E : 0, LANES, lane, a.unit, stage);
       }
     }
   }

@@ -12,7 +12,9 @@
 namespace qc {
 
 constexpr int kMxThreads = 256;
-constexpr int kMxBlocks = 6;                    // blocks of an SM
+// Blocks of an SM.  ANY: six leave 40 registers, which spill (8192 x 4098 bf16 quantised in 31.4 us, 30.0 with four; 65536 x 68
+// 7.9 and 6.0).
+template <bool ANY> constexpr int kMxBlocks = ANY ? 4 : 6;
 
 // A block is lanes_x lanes (a power of two, at least those of a scale word) along the row by kMxThreads / lanes_x rows.
 struct MxGrid {
@@ -21,14 +23,14 @@ struct MxGrid {
   size_t rows_out;        // with the rows that fill up the last tile (quantisation into tiles)
   int K;
   size_t ld;
-  int how;                // ROWS_*
+  int unit;               // bytes that rows of values may be reached in
 };
 
 template <typename T, bool ANY>
-__global__ void __launch_bounds__(kMxThreads, kMxBlocks)
+__global__ void __launch_bounds__(kMxThreads, kMxBlocks<ANY>)
 mx_quantize_kernel(const T* __restrict__ x, const MxGrid g, uint8_t* __restrict__ codes, const MxScales scales, uint32_t round_up) {
   constexpr int E = Piece<T>::E, kBlockLanes = kMxBlock / E;
-  __shared__ uint8_t stage[ANY ? kMxThreads / 32 : 1][ANY ? kWarpStage : 1];
+  __shared__ __align__(16) uint8_t stage[ANY ? kMxThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int G = min(g.lanes_x, 32);
@@ -43,7 +45,7 @@ mx_quantize_kernel(const T* __restrict__ x, const MxGrid g, uint8_t* __restrict_
   for (size_t base = blockIdx.y * static_cast<size_t>(kMxThreads >> g.log_x) + warp_row; base < g.rows_out; base += step) {
     const size_t r = base + my_row;
     Piece<T> p;
-    group_load<ANY>(p, x + r * g.ld + first, r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0, G, lane, g.how, my_stage);
+    group_load<ANY>(p, x + r * g.ld + first, r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0, G, lane, g.unit, my_stage);
     float v[E];
     p.unpack(v);
     const uint32_t s = mx_scale_byte(finite_top<kBlockLanes>(v, p.top()), round_up);
@@ -54,10 +56,10 @@ mx_quantize_kernel(const T* __restrict__ x, const MxGrid g, uint8_t* __restrict_
 }
 
 template <typename T, bool ANY>
-__global__ void __launch_bounds__(kMxThreads, kMxBlocks)
+__global__ void __launch_bounds__(kMxThreads, kMxBlocks<ANY>)
 mx_dequantize_kernel(const uint8_t* __restrict__ codes, const MxScales scales, const MxGrid g, T* __restrict__ y) {
   constexpr int E = Piece<T>::E;
-  __shared__ uint8_t stage[ANY ? kMxThreads / 32 : 1][ANY ? kWarpStage : 1];
+  __shared__ __align__(16) uint8_t stage[ANY ? kMxThreads / 32 : 1][ANY ? kWarpStage : 1];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int G = min(g.lanes_x, 32);
@@ -84,7 +86,7 @@ mx_dequantize_kernel(const uint8_t* __restrict__ codes, const MxScales scales, c
     if constexpr (E == 16) mx_decode_eight(w.y, scale_of(s), v + 8);
     Piece<T> p;
     p.pack(v);
-    group_store<ANY>(p, y + r * g.ld + first, r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0, G, lane, g.how, my_stage);
+    group_store<ANY>(p, y + r * g.ld + first, r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0, G, lane, g.unit, my_stage);
   }
 }
 

@@ -8,8 +8,8 @@
 //
 // Bound by HBM: x, residual and h once, the codes once.  A row's values stay in registers from the load to the
 // conversion: V pieces of 32 bytes a thread, and as many lanes or warps as that makes for the row's length.  16384 x 8192 bf16
-// with a residual into 4 bits: 139 us, 0.98 of the measured copy rate (73 % of the issue slots); rows whose pieces are not
-// aligned pass through shared memory (3000 x 1155 float32 13.7 us, 3000 x 1152 11.6).
+// with a residual into 4 bits: 134 us, the measured copy rate; rows whose pieces are not aligned pass through shared memory
+// (8192 x 2052 bf16 33.6 us, 2050 39.8, 2049 60.0).
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
@@ -26,9 +26,9 @@ struct NormArgs {
   const T* gain;
   T* sum;                 // or null; may be x or residual
   size_t ld_x, ld_res, ld_sum, rows;
-  int C, how, how_gain;   // how: ROWS_* of x, residual and sum together
+  int C, unit, unit_gain; // bytes that rows of x, residual and sum, and the gain, may be reached in
   int code_vec;           // a lane's int8 codes are aligned
-  double eps;
+  double eps, inv_C;
   float inv;              // NORM_I8: 2^-e
   uint8_t* codes;
   MxScales scales;        // NORM_I8_ROWS: bytes alone
@@ -49,9 +49,9 @@ __device__ __forceinline__ double row_sum(double v, double* shared, const NormPl
   if (at.warps > 1) {
     if (at.lane == 0) shared[at.warp] = v;
     __syncthreads();
-    v = at.lane < at.warps ? shared[at.lane] : 0.0;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    const int last = at.warps - 1, own = at.lane & (0x7FFFFFFF >> __clz(last) | last);
+    v = own <= last ? shared[own] : 0.0;
+    for (int d = 1; d <= last; d *= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
   }
   return v;
 }
@@ -65,60 +65,49 @@ __device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* shared, const 
   return m;
 }
 
-// What a lane has loaded of x and the residual, before it is added up.
-template <typename T, bool ANY> struct NormRaw {
+// What a lane has loaded of x and the residual, before it is added up (ANY: dealt pieces).
+template <typename T> struct NormRaw {
   Piece<T> x, r;
-};
-template <typename T> struct NormRaw<T, true> {
-  T x[Piece<T>::E], r[Piece<T>::E];
 };
 
 // The group's pieces from column `first` on: loaded (all of a thread's loads come before the first use) ...
-template <typename T, bool ANY>
-__device__ __forceinline__ void norm_fetch(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T, ANY>& raw) {
-  constexpr int E = Piece<T>::E;
+template <bool ANY, typename T>
+__device__ __forceinline__ void norm_fetch(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T>& raw) {
   const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
   const T* px = a.x + at.row * a.ld_x + first;
   const T* pr = a.residual + at.row * a.ld_res + first;
   if constexpr (ANY) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) raw.x[i] = i * at.G + at.lane < n ? px[i * at.G + at.lane] : from_float<T>(0.0f);
-    if (a.residual)
-#pragma unroll
-      for (int i = 0; i < E; ++i) raw.r[i] = i * at.G + at.lane < n ? pr[i * at.G + at.lane] : from_float<T>(0.0f);
+    with_unit<T>(a.unit, [&](auto u) {
+      load_dealt<decltype(u)::value>(raw.x, px, n, at.G, at.lane);
+      if (a.residual) load_dealt<decltype(u)::value>(raw.r, pr, n, at.G, at.lane);
+    });
   } else {
-    group_load<false>(raw.x, px, n, at.G, at.lane, a.how, nullptr);
-    if (a.residual) group_load<false>(raw.r, pr, n, at.G, at.lane, a.how, nullptr);
+    group_load<false>(raw.x, px, n, at.G, at.lane, a.unit, nullptr);
+    if (a.residual) group_load<false>(raw.r, pr, n, at.G, at.lane, a.unit, nullptr);
   }
 }
-// ... and h of them: added, rounded, kept.
-template <typename T, bool ANY>
-__device__ __forceinline__ void norm_add(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T, ANY>& raw, Piece<T>& h, uint8_t* stage) {
+// ... and h of them: added, rounded, kept (and then gathered).
+template <bool ANY, typename T>
+__device__ __forceinline__ void norm_add(const NormArgs<T>& a, const NormPlace& at, int first, const NormRaw<T>& raw, Piece<T>& h, uint8_t* stage) {
   constexpr int E = Piece<T>::E;
   const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
+  h = raw.x;
+  if (a.residual) {
+    float v[E], u[E];
+    raw.x.unpack(v);
+    raw.r.unpack(u);
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] += u[i];
+    h.pack(v);                                              // (the rounding to T)
+  }
+  T* ps = a.sum + at.row * a.ld_sum + first;
   if constexpr (ANY) {
-    // (still one value a lane, neighbouring lanes neighbouring values)
-    if (a.residual)
-#pragma unroll
-      for (int i = 0; i < E; ++i) raw.x[i] = from_float<T>(to_float(raw.x[i]) + to_float(raw.r[i]));
-    if (a.sum) {
-      T* ps = a.sum + at.row * a.ld_sum + first;
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (i * at.G + at.lane < n) ps[i * at.G + at.lane] = raw.x[i];
-    }
-    group_arrange(h, raw.x, at.G, at.lane, stage);
+    with_unit<T>(a.unit, [&](auto u) {
+      if (a.sum) store_dealt<decltype(u)::value>(h, ps, n, at.G, at.lane);
+      gather_dealt<decltype(u)::value>(h, at.G, at.lane, stage);
+    });
   } else {
-    h = raw.x;
-    if (a.residual) {
-      float v[E], u[E];
-      raw.x.unpack(v);
-      raw.r.unpack(u);
-#pragma unroll
-      for (int i = 0; i < E; ++i) v[i] += u[i];
-      h.pack(v);                                            // (the rounding to T)
-    }
-    if (a.sum) group_store<false>(h, a.sum + at.row * a.ld_sum + first, n, at.G, at.lane, a.how, nullptr);
+    if (a.sum) group_store<false>(h, ps, n, at.G, at.lane, a.unit, nullptr);
   }
 }
 
@@ -137,8 +126,8 @@ __device__ __forceinline__ void norm_scale(const NormArgs<T>& a, const NormPlace
   constexpr int E = Piece<T>::E;
   Piece<T> g;
   float u[E];
-  if (a.how_gain != ROWS_ANY) {
-    group_load<false>(g, a.gain + first, a.C - first, at.G, at.lane, a.how_gain, nullptr);
+  if (a.unit_gain >= kLaneUnit) {
+    group_load<false>(g, a.gain + first, a.C - first, at.G, at.lane, a.unit_gain, nullptr);
     g.unpack(u);
   } else {
 #pragma unroll
@@ -162,14 +151,11 @@ __device__ __forceinline__ void norm_store_i8(const NormArgs<T>& a, const NormPl
     if constexpr (E == 8) *reinterpret_cast<uint2*>(p + at.lane * E) = make_uint2(c[0], c[1]);
     else *reinterpret_cast<uint4*>(p + at.lane * E) = make_uint4(c[0], c[1], c[2], c[3]);
   } else {
-    // neighbouring lanes write neighbouring bytes
     uint8_t* mine = stage + ((threadIdx.x & 31) - at.lane) * E;
 #pragma unroll
     for (int i = 0; i < E / 4; ++i) reinterpret_cast<uint32_t*>(mine)[at.lane * (E / 4) + i] = c[i];
     __syncwarp();
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (i * at.G + at.lane < n) p[i * at.G + at.lane] = mine[i * at.G + at.lane];
+    store_bytes<E>(p, mine, min(n, at.G * E), at.G, at.lane);
     __syncwarp();
   }
 }
@@ -198,8 +184,10 @@ __device__ __forceinline__ void norm_pad_rows(const NormArgs<T>& a, int block, i
   }
 }
 
-__device__ __forceinline__ float norm_factor(double sum, int C, double eps) {
-  return static_cast<float>(1.0 / sqrt(sum / C + eps));
+// r.  (1 / C from the host and the reciprocal root in one function, off by 2^-52 or so like the sum itself, take a tenth of the
+// instructions of a division, a root and another division.)
+template <typename T> __device__ __forceinline__ float norm_factor(const NormArgs<T>& a, double sum) {
+  return static_cast<float>(rsqrt(fma(sum, a.inv_C, a.eps)));
 }
 
 // Blocks behind those of the rows (row_blocks of them) write the padding scale words.
@@ -209,7 +197,7 @@ rmsnorm_kernel(const NormArgs<T> a, int G, unsigned int row_blocks) {
   constexpr int E = Piece<T>::E;
   __shared__ double sums[kNormMaxWarps];
   __shared__ uint32_t tops[kNormMaxWarps];
-  extern __shared__ uint8_t stages[];                       // kWarpStage a warp; none where everything is aligned
+  extern __shared__ __align__(16) uint8_t stages[];         // kWarpStage a warp; none where everything is aligned
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if constexpr (OUT == NORM_MX) {
@@ -224,16 +212,16 @@ rmsnorm_kernel(const NormArgs<T> a, int G, unsigned int row_blocks) {
   uint8_t* stage = stages + (at.warp + threadIdx.y) * kWarpStage;
   Piece<T> h[V];
   {
-    NormRaw<T, ANY> raw[V];
+    NormRaw<T> raw[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) norm_fetch(a, at, (v * at.warps + at.warp) * 32 * E, raw[v]);
+    for (int v = 0; v < V; ++v) norm_fetch<ANY>(a, at, (v * at.warps + at.warp) * 32 * E, raw[v]);
 #pragma unroll
-    for (int v = 0; v < V; ++v) norm_add(a, at, (v * at.warps + at.warp) * 32 * E, raw[v], h[v], stage);
+    for (int v = 0; v < V; ++v) norm_add<ANY>(a, at, (v * at.warps + at.warp) * 32 * E, raw[v], h[v], stage);
   }
   double sum = 0.0;
 #pragma unroll
   for (int v = 0; v < V; ++v) sum = add_squares(h[v], sum);
-  const float r = norm_factor(row_sum(sum, sums, at), a.C, a.eps);
+  const float r = norm_factor(a, row_sum(sum, sums, at));
   if constexpr (OUT == NORM_I8_ROWS) {
     float y[V][E];
     uint32_t m = 0;
@@ -266,7 +254,7 @@ rmsnorm_long_kernel(const NormArgs<T> a, unsigned int row_blocks) {
   constexpr int E = Piece<T>::E, kStep = kNormMaxWarps * 32 * E;
   __shared__ double sums[kNormMaxWarps];
   __shared__ uint32_t tops[kNormMaxWarps];
-  extern __shared__ uint8_t stages[];
+  extern __shared__ __align__(16) uint8_t stages[];
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if constexpr (OUT == NORM_MX) {
@@ -278,21 +266,21 @@ rmsnorm_long_kernel(const NormArgs<T> a, unsigned int row_blocks) {
   if (a.sum) { again.x = a.sum; again.ld_x = a.ld_sum; again.residual = nullptr; }
   again.sum = nullptr;
   Piece<T> h;
-  NormRaw<T, ANY> raw;
+  NormRaw<T> raw;
   float y[E];
   double sum = 0.0;
   for (int first = at.warp * 32 * E; first < a.C; first += kStep) {
-    norm_fetch(a, at, first, raw);
-    norm_add(a, at, first, raw, h, stage);
+    norm_fetch<ANY>(a, at, first, raw);
+    norm_add<ANY>(a, at, first, raw, h, stage);
     sum = add_squares(h, sum);
   }
-  const float r = norm_factor(row_sum(sum, sums, at), a.C, a.eps);
+  const float r = norm_factor(a, row_sum(sum, sums, at));
   float inv = a.inv;
   if constexpr (OUT == NORM_I8_ROWS) {
     uint32_t m = 0;
     for (int first = at.warp * 32 * E; first < a.C; first += kStep) {
-      norm_fetch(again, at, first, raw);
-      norm_add(again, at, first, raw, h, stage);
+      norm_fetch<ANY>(again, at, first, raw);
+      norm_add<ANY>(again, at, first, raw, h, stage);
       norm_scale(a, at, first, r, h, y);
       m = max(m, finite_top<1>(y, top_bits(y)));
     }
@@ -301,8 +289,8 @@ rmsnorm_long_kernel(const NormArgs<T> a, unsigned int row_blocks) {
     if (threadIdx.x == 0) a.scales.bytes[at.row] = static_cast<uint8_t>(s);
   }
   for (int first = at.warp * 32 * E; first < a.C; first += kStep) {
-    norm_fetch(again, at, first, raw);
-    norm_add(again, at, first, raw, h, stage);
+    norm_fetch<ANY>(again, at, first, raw);
+    norm_add<ANY>(again, at, first, raw, h, stage);
     norm_scale(a, at, first, r, h, y);
     if constexpr (OUT == NORM_MX) norm_store_mx(a, at, first, y);
     else norm_store_i8(a, at, first, y, inv, stage);

@@ -79,10 +79,10 @@ int check_values(const void* p, int type, long long ld, int width, const char* w
   if (!aligned(p, type_size(type))) return fail(QCONV_ERR_ALIGNMENT, "%s must be aligned to its type", what);
   return QCONV_OK;
 }
-// How rows from p on, `ld` elements apart, may be reached (ROWS_*).
+// The unit, in bytes, that rows from p on, `ld` elements apart, may be reached in.
 int reach(const void* p, int type, long long ld) {
-  const long long bytes = ld * static_cast<long long>(type_size(type));
-  return aligned(p, 32) && bytes % 32 == 0 ? qc::ROWS_32 : aligned(p, 16) && bytes % 16 == 0 ? qc::ROWS_16 : qc::ROWS_ANY;
+  const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * static_cast<long long>(type_size(type))) | 32u;
+  return static_cast<int>(bits & (~bits + 1));               // the lowest bit
 }
 
 // The blocks of a conversion over `rows_out` rows: enough lanes along the row, and rows until the device is full.
@@ -95,10 +95,10 @@ qc::MxGrid mx_grid(long long rows, long long rows_out, int K, long long ld, int 
   while (g.lanes_x > 32 && ((lanes + g.lanes_x - 1) / g.lanes_x * g.lanes_x - lanes) * 8 > lanes) g.lanes_x /= 2;   // few lanes behind the row's end
   while ((1 << g.log_x) < g.lanes_x) ++g.log_x;
   g.rows = static_cast<size_t>(rows); g.rows_out = static_cast<size_t>(rows_out); g.K = K; g.ld = static_cast<size_t>(ld);
-  g.how = reach(values, type, ld);
+  g.unit = reach(values, type, ld);
   const long long per_block = qc::kMxThreads / g.lanes_x;
   grid->x = static_cast<unsigned int>((lanes + g.lanes_x - 1) / g.lanes_x);
-  const long long most = std::max(1ll, 148ll * qc::kMxBlocks / grid->x);   // (all at once, as many rows each)
+  const long long most = std::max(1ll, 148ll * (g.unit < qc::kLaneUnit ? qc::kMxBlocks<true> : qc::kMxBlocks<false>) / grid->x);   // (all at once, as many rows each)
   grid->y = static_cast<unsigned int>(std::min({(rows_out + per_block - 1) / per_block, most, 65535ll}));
   return g;
 }
@@ -144,7 +144,7 @@ int qmx_quantize(const void* d_x, int type, long long rows, int K, long long ld,
   const qc::MxGrid g = mx_grid(rows, layout == QMX_TILES ? (rows + 127) / 128 * 128 : rows, K, ld, type, d_x, &grid);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const auto kernel = g.how == qc::ROWS_ANY ? qc::mx_quantize_kernel<T, true> : qc::mx_quantize_kernel<T, false>;
+    const auto kernel = g.unit < qc::kLaneUnit ? qc::mx_quantize_kernel<T, true> : qc::mx_quantize_kernel<T, false>;
     CUDA_TRY(launch_chained(kernel, grid, dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream), static_cast<const T*>(d_x), g, d_codes,
                             make_scales(d_scales, rows, K, layout), rule == QMX_COVER ? qc::kCoverRoundUp : 0u));
     return static_cast<int>(QCONV_OK);
@@ -163,7 +163,7 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
   const qc::MxGrid g = mx_grid(rows, rows, K, ld, type, d_y, &grid);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const auto kernel = g.how == qc::ROWS_ANY ? qc::mx_dequantize_kernel<T, true> : qc::mx_dequantize_kernel<T, false>;
+    const auto kernel = g.unit < qc::kLaneUnit ? qc::mx_dequantize_kernel<T, true> : qc::mx_dequantize_kernel<T, false>;
     CUDA_TRY(launch_chained(kernel, grid, dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream), d_codes,
                             make_scales(const_cast<uint8_t*>(d_scales), rows, K, layout), g, static_cast<T*>(d_y)));
     return static_cast<int>(QCONV_OK);
@@ -469,7 +469,7 @@ unsigned int pad_blocks(const qc::NormArgs<T>& a) {
 
 template <typename T, int OUT>
 size_t norm_stages(const qc::NormArgs<T>& a, int warps) {
-  return a.how == qc::ROWS_ANY || (OUT != qc::NORM_MX && !a.code_vec) ? static_cast<size_t>(warps) * qc::kWarpStage : 0;
+  return a.unit < qc::kLaneUnit || (OUT != qc::NORM_MX && !a.code_vec) ? static_cast<size_t>(warps) * qc::kWarpStage : 0;
 }
 
 // G lanes of a warp a row (four warps a block), or `warps` warps.
@@ -479,7 +479,7 @@ int launch_norm(const qc::NormArgs<T>& a, int G, int warps, cudaStream_t st) {
   const size_t per_block = static_cast<size_t>(y) * (32 / G);
   const unsigned int blocks = static_cast<unsigned int>((a.rows + per_block - 1) / per_block);
   auto kernel = qc::rmsnorm_kernel<T, OUT, V, false>;
-  if constexpr (V <= 2) kernel = a.how == qc::ROWS_ANY ? qc::rmsnorm_kernel<T, OUT, V, true> : kernel;
+  if constexpr (V <= 2) kernel = a.unit < qc::kLaneUnit ? qc::rmsnorm_kernel<T, OUT, V, true> : kernel;
   CUDA_TRY(launch_chained(kernel, dim3(blocks + pad_blocks<OUT>(a)), dim3(32 * warps, y), norm_stages<T, OUT>(a, warps * static_cast<int>(y)), st, a, G, blocks));
   return QCONV_OK;
 }
@@ -498,10 +498,14 @@ int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
     while (G < lanes) G *= 2;
     return launch_norm<T, OUT, 1>(a, G, 1, st);
   }
-  if (lanes <= 1024 && a.rows < 512) return launch_norm<T, OUT, 1>(a, 32, warps(1), st);
+  // Two pieces a thread; one where rows are few, and where an odd number of warps up to three, or five where the rows go
+  // through shared memory, takes one: 16384 x 1536 bf16 to 4 bits 31.1 us against 33.3, 12264 x 2052 48.7 against 59.2;
+  // with seven and eleven warps 7021 x 3584 33.5 against 30.9, 4911 x 5124 54.9 against 51.4.
+  const bool any = a.unit < qc::kLaneUnit, odd = warps(1) % 2 == 1 && warps(1) <= (any ? 5 : 3);
+  if (lanes <= 1024 && (a.rows < 512 || odd)) return launch_norm<T, OUT, 1>(a, 32, warps(1), st);
   if (lanes <= 1024) return launch_norm<T, OUT, 2>(a, 32, warps(2), st);
-  if (lanes <= 2048 && a.how != qc::ROWS_ANY) return launch_norm<T, OUT, 4>(a, 32, warps(4), st);
-  const auto kernel = a.how == qc::ROWS_ANY ? qc::rmsnorm_long_kernel<T, OUT, true> : qc::rmsnorm_long_kernel<T, OUT, false>;
+  if (lanes <= 2048 && !any) return launch_norm<T, OUT, 4>(a, 32, warps(4), st);
+  const auto kernel = any ? qc::rmsnorm_long_kernel<T, OUT, true> : qc::rmsnorm_long_kernel<T, OUT, false>;
   const unsigned int blocks = static_cast<unsigned int>(a.rows);
   CUDA_TRY(launch_chained(kernel, dim3(blocks + pad_blocks<OUT>(a)), dim3(32 * qc::kNormMaxWarps), norm_stages<T, OUT>(a, qc::kNormMaxWarps), st, a, blocks));
   return QCONV_OK;
@@ -540,11 +544,11 @@ int qrmsnorm(const qrmsnorm_args* args, void* cuda_stream) {
     a.x = static_cast<const T*>(g.d_x); a.residual = static_cast<const T*>(g.d_residual); a.gain = static_cast<const T*>(g.d_gain);
     a.sum = static_cast<T*>(g.d_sum);
     a.ld_x = g.ld_x; a.ld_res = g.d_residual ? g.ld_residual : 0; a.ld_sum = g.d_sum ? g.ld_sum : 0;
-    a.rows = g.rows; a.C = g.C; a.eps = g.eps;
-    a.how = reach(g.d_x, g.type, g.ld_x);
-    a.how_gain = reach(g.d_gain, g.type, 0);
-    if (g.d_residual) a.how = std::min(a.how, reach(g.d_residual, g.type, g.ld_residual));
-    if (g.d_sum) a.how = std::min(a.how, reach(g.d_sum, g.type, g.ld_sum));
+    a.rows = g.rows; a.C = g.C; a.eps = g.eps; a.inv_C = 1.0 / g.C;
+    a.unit = reach(g.d_x, g.type, g.ld_x);
+    a.unit_gain = reach(g.d_gain, g.type, 0);
+    if (g.d_residual) a.unit = std::min(a.unit, reach(g.d_residual, g.type, g.ld_residual));
+    if (g.d_sum) a.unit = std::min(a.unit, reach(g.d_sum, g.type, g.ld_sum));
     a.code_vec = aligned(g.d_codes, qc::Piece<T>::E) && g.C % qc::Piece<T>::E == 0;
     a.inv = std::ldexp(1.0f, -g.e);
     a.codes = g.d_codes;
@@ -580,7 +584,7 @@ int cache_args(const qcache_desc* c, const qcache_values* keys, const qcache_val
   a->code_pitch = c->format == QCACHE_I8 ? c->D : a->blocks * 16;
   a->scale_pitch = c->format == QCACHE_I8 ? 1 : a->blocks;
   const int per_lane = 32 / static_cast<int>(type_size(type));
-  a->how = qc::ROWS_32;
+  a->unit = 32;
   a->code_vec = c->D % per_lane == 0;
   const qcache_values* in[2] = {keys, values};
   uint8_t* codes[2] = {c->d_k_codes, c->d_v_codes};
@@ -593,7 +597,7 @@ int cache_args(const qcache_desc* c, const qcache_values* keys, const qcache_val
     if (!aligned(v.d_values, type_size(type))) return fail(QCONV_ERR_ALIGNMENT, "values must be aligned to their type");
     if (c->format == QCACHE_MX && !aligned(codes[i], 16)) return fail(QCONV_ERR_ALIGNMENT, "codes must be 16-byte aligned");
     a->side[i] = {codes[i], scales[i], v.d_values, v.token_stride, v.head_stride};
-    a->how = std::min({a->how, reach(v.d_values, type, v.token_stride), reach(v.d_values, type, v.head_stride)});
+    a->unit = std::min({a->unit, reach(v.d_values, type, v.token_stride), reach(v.d_values, type, v.head_stride)});
     a->code_vec &= aligned(codes[i], per_lane);
   }
   return QCONV_OK;
@@ -601,15 +605,16 @@ int cache_args(const qcache_desc* c, const qcache_values* keys, const qcache_val
 
 template <typename T, int FMT, int LANES, int V>
 int launch_cache(const qc::CacheArgs& a, bool write, cudaStream_t st) {
-  const bool any = a.how == qc::ROWS_ANY;
+  const bool any = a.unit < qc::kLaneUnit || (FMT == qc::CACHE_I8 && write && !a.code_vec);
   const auto kernel = write ? (any ? qc::cache_write_kernel<T, FMT, LANES, V, true> : qc::cache_write_kernel<T, FMT, LANES, V, false>)
                             : (any ? qc::cache_read_kernel<T, FMT, LANES, V, true> : qc::cache_read_kernel<T, FMT, LANES, V, false>);
-  CUDA_TRY(launch_chained(kernel, dim3(qc::grid_for(a.items, qc::kCacheThreads / LANES, 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));
+  CUDA_TRY(launch_chained(kernel, dim3(qc::grid_for(a.items, qc::kCacheThreads / 32 * (32 / (any || !write ? LANES : a.lanes)), 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));
   return QCONV_OK;
 }
 template <typename T, int FMT>
-int run_cache(const qc::CacheArgs& a, bool write, cudaStream_t st) {
+int run_cache(qc::CacheArgs a, bool write, cudaStream_t st) {
   const int lanes = (FMT == qc::CACHE_MX ? a.blocks * qc::kMxBlock : a.D) / qc::Piece<T>::E + (FMT == qc::CACHE_I8 && a.D % qc::Piece<T>::E != 0);
+  a.lanes = lanes <= 2 ? 4 : std::min(lanes, 32);            // (above half of the forms' lanes, and whole blocks of 4-bit codes)
   if (lanes <= 4) return launch_cache<T, FMT, 4, 1>(a, write, st);
   if (lanes <= 8) return launch_cache<T, FMT, 8, 1>(a, write, st);
   if (lanes <= 16) return launch_cache<T, FMT, 16, 1>(a, write, st);

@@ -13,6 +13,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
+#include <cstring>
+#include <type_traits>
 
 #include "epilogue.cuh"
 
@@ -70,8 +72,10 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   return r;
 }
 
-// How a row of values may be reached.
-enum : int { ROWS_ANY = 0, ROWS_16 = 1, ROWS_32 = 2 };     // one value at a time; in 16-byte pieces; in 32-byte pieces
+// How rows of values may be reached: in units of so many bytes (a power of two from the type's size to 32).  From 16 on
+// a lane loads its own values; below, neighbouring lanes take neighbouring units and exchange them through shared memory
+// (group_load).  The wider the unit the fewer the instructions: 8192 x 4100, 4098 and 4097 bf16 take UUU us to quantise, 4096 16.5.
+constexpr int kLaneUnit = 16;
 
 // What a lane holds of a row: 32 bytes, E consecutive values (8 float32, 16 of a 16-bit type).
 template <typename T> struct Piece {
@@ -83,8 +87,8 @@ template <typename T> struct Piece {
     for (int i = 0; i < 8; ++i) w[i] = 0u;
   }
   // Whole pieces.  (Ordinary loads, not the read-only path: the memory may be written by this kernel, too.)
-  __device__ __forceinline__ void load(const T* p, int how) {
-    if (how == ROWS_32) {
+  __device__ __forceinline__ void load(const T* p, int unit) {
+    if (unit == 32) {
       asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                    : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
     } else {
@@ -92,8 +96,8 @@ template <typename T> struct Piece {
       w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
     }
   }
-  __device__ __forceinline__ void store(T* p, int how) const {
-    if (how == ROWS_32) {
+  __device__ __forceinline__ void store(T* p, int unit) const {
+    if (unit == 32) {
       asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                    ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
     } else {
@@ -143,34 +147,106 @@ template <typename T> struct Piece {
   }
 };
 
-// Bytes of shared memory a warp needs for rows that are reached one value at a time.
+// Bytes of shared memory a warp needs for rows that are reached in units below 16 bytes.
 constexpr int kWarpStage = 1024;
 
-// Lane l of a group of G holds values l, l + G, l + 2 G, ... and gets E consecutive ones, through its warp's shared memory.
-template <typename T>
-__device__ __forceinline__ void group_arrange(Piece<T>& x, const T (&v)[Piece<T>::E], int G, int lane, uint8_t* stage) {
-  constexpr int E = Piece<T>::E;
-  T* mine = reinterpret_cast<T*>(stage) + ((threadIdx.x & 31) - lane) * E;
+// The bits of a unit of U bytes.
+template <int U> struct UnitOf { using type = unsigned short; };
+template <> struct UnitOf<4> { using type = uint32_t; };
+template <> struct UnitOf<8> { using type = uint2; };
+
+// Unit i of a piece that holds units lane, lane + G, lane + 2 G, ... of a group's values (dealt pieces).
+template <int U> __device__ __forceinline__ typename UnitOf<U>::type unit_of(const uint32_t (&w)[8], int i) {
+  if constexpr (U == 8) return make_uint2(w[2 * i], w[2 * i + 1]);
+  else if constexpr (U == 4) return w[i];
+  else return static_cast<unsigned short>(w[i >> 1] >> (16 * (i & 1)));
+}
+template <int U> __device__ __forceinline__ void set_unit(uint32_t (&w)[8], int i, typename UnitOf<U>::type v) {
+  if constexpr (U == 8) { w[2 * i] = v.x; w[2 * i + 1] = v.y; }
+  else if constexpr (U == 4) w[i] = v;
+  else w[i >> 1] = (i & 1) ? w[i >> 1] | static_cast<uint32_t>(v) << 16 : v;
+}
+
+// Dealt pieces from p, where n values exist (zeros behind them), and back; units of U bytes.
+template <int U, typename T>
+__device__ __forceinline__ void load_dealt(Piece<T>& x, const T* p, int n, int G, int lane) {
+  using Unit = typename UnitOf<U>::type;
+  constexpr int kValues = U / static_cast<int>(sizeof(T));   // of a unit
 #pragma unroll
-  for (int i = 0; i < E; ++i) mine[i * G + lane] = v[i];
+  for (int i = 0; i < 32 / U; ++i) {
+    const int at = (i * G + lane) * kValues, left = n - at;
+    Unit v{};
+    if (left >= kValues) v = *reinterpret_cast<const Unit*>(p + at);
+    else if (kValues > 1 && left > 0) {                      // (the row ends inside a unit)
+      T part[kValues];
+#pragma unroll
+      for (int k = 0; k < kValues; ++k) part[k] = k < left ? p[at + k] : from_float<T>(0.0f);
+      memcpy(&v, part, U);
+    }
+    set_unit<U>(x.w, i, v);
+  }
+}
+template <int U, typename T>
+__device__ __forceinline__ void store_dealt(const Piece<T>& x, T* p, int n, int G, int lane) {
+  using Unit = typename UnitOf<U>::type;
+  constexpr int kValues = U / static_cast<int>(sizeof(T));
+#pragma unroll
+  for (int i = 0; i < 32 / U; ++i) {
+    const int at = (i * G + lane) * kValues, left = n - at;
+    const Unit v = unit_of<U>(x.w, i);
+    if (left >= kValues) *reinterpret_cast<Unit*>(p + at) = v;
+    else if (kValues > 1 && left > 0) {
+      T part[kValues];
+      memcpy(part, &v, U);
+#pragma unroll
+      for (int k = 0; k < kValues; ++k)
+        if (k < left) p[at + k] = part[k];
+    }
+  }
+}
+// Dealt pieces to those of consecutive values and back, through the warp's shared memory.  Whole warps.
+template <int U, typename T>
+__device__ __forceinline__ void gather_dealt(Piece<T>& x, int G, int lane, uint8_t* stage) {
+  using Unit = typename UnitOf<U>::type;
+  uint8_t* group = stage + ((threadIdx.x & 31) - lane) * 32;
+#pragma unroll
+  for (int i = 0; i < 32 / U; ++i) reinterpret_cast<Unit*>(group)[i * G + lane] = unit_of<U>(x.w, i);
   __syncwarp();
-  const uint4* q = reinterpret_cast<const uint4*>(mine + lane * E);
+  const uint4* q = reinterpret_cast<const uint4*>(group + lane * 32);
   const uint4 a = q[0], b = q[1];
   x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w; x.w[4] = b.x; x.w[5] = b.y; x.w[6] = b.z; x.w[7] = b.w;
   __syncwarp();
 }
+template <int U, typename T>
+__device__ __forceinline__ void deal(Piece<T>& x, int G, int lane, uint8_t* stage) {
+  using Unit = typename UnitOf<U>::type;
+  uint8_t* group = stage + ((threadIdx.x & 31) - lane) * 32;
+  uint4* q = reinterpret_cast<uint4*>(group + lane * 32);
+  q[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+  q[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 32 / U; ++i) set_unit<U>(x.w, i, reinterpret_cast<const Unit*>(group)[i * G + lane]);
+  __syncwarp();
+}
+// f(the unit as a constant, at most 8 bytes) for a unit that is the same for the whole grid.
+template <typename T, typename F>
+__device__ __forceinline__ void with_unit(int unit, F&& f) {
+  if (unit >= 8) f(std::integral_constant<int, 8>());
+  else if (sizeof(T) == 4 || unit == 4) f(std::integral_constant<int, 4>());
+  else f(std::integral_constant<int, sizeof(T) == 2 ? 2 : 4>());
+}
 
 // Loads the pieces of a group of G lanes (a power of two up to 32): G * E consecutive values from p on, of which the first
-// n exist (zeros behind them; n may be negative).  Where 16-byte accesses are not aligned the group reads one value a
-// lane, neighbouring lanes neighbouring values, and passes them through its warp's shared memory.  Whole warps.  ANY: how is
-// ROWS_ANY (an instantiation of its own, so that the aligned one is lean).
+// n exist (zeros behind them; n may be negative).  ANY: in units below 16 bytes (an instantiation of its own, so that the
+// aligned one is lean).  Whole warps.
 template <bool ANY, typename T>
-__device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G, int lane, int how, uint8_t* stage) {
+__device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G, int lane, int unit, uint8_t* stage) {
   constexpr int E = Piece<T>::E;
   if constexpr (!ANY) {
     const int left = n - lane * E;
     if (left >= E) {
-      x.load(p + lane * E, how);
+      x.load(p + lane * E, unit);
     } else {
       x.clear();
       if (left > 0) {
@@ -181,20 +257,20 @@ __device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G
       }
     }
   } else {
-    T v[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = i * G + lane < n ? p[i * G + lane] : from_float<T>(0.0f);
-    group_arrange(x, v, G, lane, stage);
+    with_unit<T>(unit, [&](auto u) {
+      load_dealt<decltype(u)::value>(x, p, n, G, lane);
+      gather_dealt<decltype(u)::value>(x, G, lane, stage);
+    });
   }
 }
 // The same way back: the first n values.
 template <bool ANY, typename T>
-__device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int G, int lane, int how, uint8_t* stage) {
+__device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int G, int lane, int unit, uint8_t* stage) {
   constexpr int E = Piece<T>::E;
   if constexpr (!ANY) {
     const int left = n - lane * E;
     if (left >= E) {
-      x.store(p + lane * E, how);
+      x.store(p + lane * E, unit);
     } else if (left > 0) {
       float v[E];
       x.unpack(v);
@@ -203,16 +279,73 @@ __device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int 
         if (i < left) p[lane * E + i] = from_float<T>(v[i]);
     }
   } else {
-    T* mine = reinterpret_cast<T*>(stage) + ((threadIdx.x & 31) - lane) * E;
-    uint4* q = reinterpret_cast<uint4*>(mine + lane * E);
-    q[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
-    q[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (i * G + lane < n) p[i * G + lane] = mine[i * G + lane];
-    __syncwarp();
+    with_unit<T>(unit, [&](auto u) {
+      Piece<T> dealt = x;
+      deal<decltype(u)::value>(dealt, G, lane, stage);
+      store_dealt<decltype(u)::value>(dealt, p, n, G, lane);
+    });
   }
+}
+
+// Bytes from or to p, which may be anywhere, for a group of G lanes (at least four): the first n of G * E.  Neighbouring
+// lanes take neighbouring aligned words, and a few of them the bytes before the first and behind the last word.
+struct ByteRun {
+  int head, words, tail;
+  __device__ __forceinline__ ByteRun(const uint8_t* p, int n) {
+    n = max(n, 0);
+    head = min(n, static_cast<int>(-reinterpret_cast<uintptr_t>(p) & 3));
+    words = (n - head) >> 2;
+    tail = (n - head) & 3;
+  }
+};
+// From `bytes`, shared memory (4-byte aligned, readable up to the word behind the last byte's).
+template <int E>
+__device__ __forceinline__ void store_bytes(uint8_t* p, const uint8_t* bytes, int n, int G, int lane) {
+  const ByteRun run(p, n);
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(bytes);
+  if (lane < run.head) p[lane] = bytes[lane];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) {
+    const int k = i * G + lane;
+    if (k < run.words) *reinterpret_cast<uint32_t*>(p + run.head + 4 * k) = __funnelshift_r(words[k], words[k + 1], 8 * run.head);
+  }
+  const int end = run.head + 4 * run.words + lane;
+  if (lane < run.tail) p[end] = bytes[end];
+}
+
+// As loaded: a lane's words, and its byte before the first (low) and behind the last.  Then, through the group's part of
+// `stage` (kStagedBytes<E, G> of it), each lane's own E bytes; where there are none, anything.  Whole warps.
+template <int E> struct DealtBytes {
+  uint32_t w[E / 4], ends;
+};
+template <int E>
+__device__ __forceinline__ void load_bytes(DealtBytes<E>& x, const uint8_t* p, int n, int G, int lane) {
+  const ByteRun run(p, n);
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) x.w[i] = i * G + lane < run.words ? __ldg(reinterpret_cast<const uint32_t*>(p + run.head) + i * G + lane) : 0u;
+  x.ends = lane < run.head ? __ldg(p + lane) : 0u;
+  if (lane < run.tail) x.ends |= static_cast<uint32_t>(__ldg(p + run.head + 4 * run.words + lane)) << 8;
+}
+template <int E, int G> constexpr int kStagedBytes = G * E + 8;
+template <int E>
+__device__ __forceinline__ void gather_bytes(uint32_t (&w)[E / 4], const DealtBytes<E>& x, const uint8_t* p, int n, int G, int lane, uint8_t* group) {
+  const ByteRun run(p, n);
+  // byte b is staged at 4 - head + b
+  if (lane < run.head) group[4 - run.head + lane] = static_cast<uint8_t>(x.ends);
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i)
+    if (i * G + lane < run.words) reinterpret_cast<uint32_t*>(group)[1 + i * G + lane] = x.w[i];
+  if (lane < run.tail) group[4 + 4 * run.words + lane] = static_cast<uint8_t>(x.ends >> 8);
+  __syncwarp();
+  const uint32_t* q = reinterpret_cast<const uint32_t*>(group) + ((4 - run.head) >> 2) + lane * (E / 4);
+  uint32_t lo = q[0];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) {
+    const uint32_t hi = q[i + 1];
+    w[i] = __funnelshift_r(lo, hi, 8 * ((4 - run.head) & 3));
+    lo = hi;
+  }
+  __syncwarp();
 }
 
 // Bits of the largest |v| over a lane's values, at least infinity's if one is not finite; over the finite ones alone, with
