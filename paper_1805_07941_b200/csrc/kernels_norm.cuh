@@ -126,7 +126,7 @@ __device__ __forceinline__ void norm_scale(const NormArgs<T>& a, const NormPlace
   constexpr int E = Piece<T>::E;
   Piece<T> g;
   float u[E];
-  if (a.unit_gain >= kLaneUnit) {
+  if (a.unit_gain >= kLoadUnit) {
     group_load<false>(g, a.gain + first, a.C - first, at.G, at.lane, a.unit_gain, nullptr);
     g.unpack(u);
   } else {

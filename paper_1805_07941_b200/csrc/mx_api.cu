@@ -85,8 +85,9 @@ int reach(const void* p, int type, long long ld) {
   return static_cast<int>(bits & (~bits + 1));               // the lowest bit
 }
 
-// The blocks of a conversion over `rows_out` rows: enough lanes along the row, and rows until the device is full.
-qc::MxGrid mx_grid(long long rows, long long rows_out, int K, long long ld, int type, const void* values, dim3* grid) {
+// The blocks of a conversion over `rows_out` rows: enough lanes along the row, and rows until the device is full.  any: lanes
+// exchange values, as units below `own` bytes need it.
+qc::MxGrid mx_grid(long long rows, long long rows_out, int K, long long ld, int type, const void* values, int own, dim3* grid, bool* any) {
   const int E = 32 / static_cast<int>(type_size(type));
   const int lanes = qc::mx_blocks(K) * (qc::kMxBlock / E);
   qc::MxGrid g = {};
@@ -96,9 +97,10 @@ qc::MxGrid mx_grid(long long rows, long long rows_out, int K, long long ld, int 
   while ((1 << g.log_x) < g.lanes_x) ++g.log_x;
   g.rows = static_cast<size_t>(rows); g.rows_out = static_cast<size_t>(rows_out); g.K = K; g.ld = static_cast<size_t>(ld);
   g.unit = reach(values, type, ld);
+  *any = g.unit < own;
   const long long per_block = qc::kMxThreads / g.lanes_x;
   grid->x = static_cast<unsigned int>((lanes + g.lanes_x - 1) / g.lanes_x);
-  const long long most = std::max(1ll, 148ll * (g.unit < qc::kLaneUnit ? qc::kMxBlocks<true> : qc::kMxBlocks<false>) / grid->x);   // (all at once, as many rows each)
+  const long long most = std::max(1ll, 148ll * (*any ? qc::kMxBlocks<true> : qc::kMxBlocks<false>) / grid->x);   // (all at once, as many rows each)
   grid->y = static_cast<unsigned int>(std::min({(rows_out + per_block - 1) / per_block, most, 65535ll}));
   return g;
 }
@@ -141,10 +143,11 @@ int qmx_quantize(const void* d_x, int type, long long rows, int K, long long ld,
   if (!rc) rc = check_code_alignment(d_codes, d_scales, layout);
   if (rc) return rc;
   dim3 grid;
-  const qc::MxGrid g = mx_grid(rows, layout == QMX_TILES ? (rows + 127) / 128 * 128 : rows, K, ld, type, d_x, &grid);
+  bool any;
+  const qc::MxGrid g = mx_grid(rows, layout == QMX_TILES ? (rows + 127) / 128 * 128 : rows, K, ld, type, d_x, qc::kLoadUnit, &grid, &any);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const auto kernel = g.unit < qc::kLaneUnit ? qc::mx_quantize_kernel<T, true> : qc::mx_quantize_kernel<T, false>;
+    const auto kernel = any ? qc::mx_quantize_kernel<T, true> : qc::mx_quantize_kernel<T, false>;
     CUDA_TRY(launch_chained(kernel, grid, dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream), static_cast<const T*>(d_x), g, d_codes,
                             make_scales(d_scales, rows, K, layout), rule == QMX_COVER ? qc::kCoverRoundUp : 0u));
     return static_cast<int>(QCONV_OK);
@@ -160,10 +163,11 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
   if (!rc) rc = check_code_alignment(d_codes, d_scales, layout);
   if (rc) return rc;
   dim3 grid;
-  const qc::MxGrid g = mx_grid(rows, rows, K, ld, type, d_y, &grid);
+  bool any;
+  const qc::MxGrid g = mx_grid(rows, rows, K, ld, type, d_y, qc::kStoreUnit, &grid, &any);
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    const auto kernel = g.unit < qc::kLaneUnit ? qc::mx_dequantize_kernel<T, true> : qc::mx_dequantize_kernel<T, false>;
+    const auto kernel = any ? qc::mx_dequantize_kernel<T, true> : qc::mx_dequantize_kernel<T, false>;
     CUDA_TRY(launch_chained(kernel, grid, dim3(qc::kMxThreads), 0, static_cast<cudaStream_t>(cuda_stream), d_codes,
                             make_scales(const_cast<uint8_t*>(d_scales), rows, K, layout), g, static_cast<T*>(d_y)));
     return static_cast<int>(QCONV_OK);
@@ -469,7 +473,7 @@ unsigned int pad_blocks(const qc::NormArgs<T>& a) {
 
 template <typename T, int OUT>
 size_t norm_stages(const qc::NormArgs<T>& a, int warps) {
-  return a.unit < qc::kLaneUnit || (OUT != qc::NORM_MX && !a.code_vec) ? static_cast<size_t>(warps) * qc::kWarpStage : 0;
+  return a.unit < qc::kLoadUnit || (OUT != qc::NORM_MX && !a.code_vec) ? static_cast<size_t>(warps) * qc::kWarpStage : 0;
 }
 
 // G lanes of a warp a row (four warps a block), or `warps` warps.
@@ -479,7 +483,7 @@ int launch_norm(const qc::NormArgs<T>& a, int G, int warps, cudaStream_t st) {
   const size_t per_block = static_cast<size_t>(y) * (32 / G);
   const unsigned int blocks = static_cast<unsigned int>((a.rows + per_block - 1) / per_block);
   auto kernel = qc::rmsnorm_kernel<T, OUT, V, false>;
-  if constexpr (V <= 2) kernel = a.unit < qc::kLaneUnit ? qc::rmsnorm_kernel<T, OUT, V, true> : kernel;
+  if constexpr (V <= 2) kernel = a.unit < qc::kLoadUnit ? qc::rmsnorm_kernel<T, OUT, V, true> : kernel;
   CUDA_TRY(launch_chained(kernel, dim3(blocks + pad_blocks<OUT>(a)), dim3(32 * warps, y), norm_stages<T, OUT>(a, warps * static_cast<int>(y)), st, a, G, blocks));
   return QCONV_OK;
 }
@@ -501,7 +505,7 @@ int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
   // Two pieces a thread; one where rows are few, and where an odd number of warps up to three, or five where the rows go
   // through shared memory, takes one: 16384 x 1536 bf16 to 4 bits 31.1 us against 33.3, 12264 x 2052 48.7 against 59.2;
   // with seven and eleven warps 7021 x 3584 33.5 against 30.9, 4911 x 5124 54.9 against 51.4.
-  const bool any = a.unit < qc::kLaneUnit, odd = warps(1) % 2 == 1 && warps(1) <= (any ? 5 : 3);
+  const bool any = a.unit < qc::kLoadUnit, odd = warps(1) % 2 == 1 && warps(1) <= (any ? 5 : 3);
   if (lanes <= 1024 && (a.rows < 512 || odd)) return launch_norm<T, OUT, 1>(a, 32, warps(1), st);
   if (lanes <= 1024) return launch_norm<T, OUT, 2>(a, 32, warps(2), st);
   if (lanes <= 2048 && !any) return launch_norm<T, OUT, 4>(a, 32, warps(4), st);
@@ -605,7 +609,7 @@ int cache_args(const qcache_desc* c, const qcache_values* keys, const qcache_val
 
 template <typename T, int FMT, int LANES, int V>
 int launch_cache(const qc::CacheArgs& a, bool write, cudaStream_t st) {
-  const bool any = a.unit < qc::kLaneUnit || (FMT == qc::CACHE_I8 && write && !a.code_vec);
+  const bool any = write ? a.unit < qc::kLoadUnit || (FMT == qc::CACHE_I8 && !a.code_vec) : a.unit < qc::kStoreUnit;
   const auto kernel = write ? (any ? qc::cache_write_kernel<T, FMT, LANES, V, true> : qc::cache_write_kernel<T, FMT, LANES, V, false>)
                             : (any ? qc::cache_read_kernel<T, FMT, LANES, V, true> : qc::cache_read_kernel<T, FMT, LANES, V, false>);
   CUDA_TRY(launch_chained(kernel, dim3(qc::grid_for(a.items, qc::kCacheThreads / 32 * (32 / (any || !write ? LANES : a.lanes)), 148 * 8)), dim3(qc::kCacheThreads), 0, st, a));

@@ -72,10 +72,12 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   return r;
 }
 
-// How rows of values may be reached: in units of so many bytes (a power of two from the type's size to 32).  From 16 on
-// a lane loads its own values; below, neighbouring lanes take neighbouring units and exchange them through shared memory
-// (group_load).  The wider the unit the fewer the instructions: 8192 x 4100, 4098 and 4097 bf16 take UUU us to quantise, 4096 16.5.
-constexpr int kLaneUnit = 16;
+// How rows of values may be reached: in units of so many bytes (a power of two from the type's size to 32).  From kLoadUnit
+// on (loads) or kStoreUnit (stores) a lane moves its own values; below, neighbouring lanes take neighbouring units and
+// exchange them through shared memory (group_load).  8192 rows of 4096, 4100, 4098, 4097 bf16 take 16.5, 26.0, 30.0, 35 us to
+// quantise.  Units of 16 bytes, own and exchanged: 8192 x 4100 float32 quantised in 28.9 and 39.1 us, read back in 41.8 and
+// 35.9; 65536 x 72 bf16 6.3 and 6.2, back 8.9 and 5.6 (two stores a lane, each of parts of sectors).
+constexpr int kLoadUnit = 16, kStoreUnit = 32;
 
 // What a lane holds of a row: 32 bytes, E consecutive values (8 float32, 16 of a 16-bit type).
 template <typename T> struct Piece {
@@ -154,15 +156,18 @@ constexpr int kWarpStage = 1024;
 template <int U> struct UnitOf { using type = unsigned short; };
 template <> struct UnitOf<4> { using type = uint32_t; };
 template <> struct UnitOf<8> { using type = uint2; };
+template <> struct UnitOf<16> { using type = uint4; };
 
 // Unit i of a piece that holds units lane, lane + G, lane + 2 G, ... of a group's values (dealt pieces).
 template <int U> __device__ __forceinline__ typename UnitOf<U>::type unit_of(const uint32_t (&w)[8], int i) {
-  if constexpr (U == 8) return make_uint2(w[2 * i], w[2 * i + 1]);
+  if constexpr (U == 16) return make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  else if constexpr (U == 8) return make_uint2(w[2 * i], w[2 * i + 1]);
   else if constexpr (U == 4) return w[i];
   else return static_cast<unsigned short>(w[i >> 1] >> (16 * (i & 1)));
 }
 template <int U> __device__ __forceinline__ void set_unit(uint32_t (&w)[8], int i, typename UnitOf<U>::type v) {
-  if constexpr (U == 8) { w[2 * i] = v.x; w[2 * i + 1] = v.y; }
+  if constexpr (U == 16) { w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w; }
+  else if constexpr (U == 8) { w[2 * i] = v.x; w[2 * i + 1] = v.y; }
   else if constexpr (U == 4) w[i] = v;
   else w[i >> 1] = (i & 1) ? w[i >> 1] | static_cast<uint32_t>(v) << 16 : v;
 }
@@ -229,16 +234,17 @@ __device__ __forceinline__ void deal(Piece<T>& x, int G, int lane, uint8_t* stag
   for (int i = 0; i < 32 / U; ++i) set_unit<U>(x.w, i, reinterpret_cast<const Unit*>(group)[i * G + lane]);
   __syncwarp();
 }
-// f(the unit as a constant, at most 8 bytes) for a unit that is the same for the whole grid.
+// f(the unit as a constant, at most 16 bytes) for a unit that is the same for the whole grid.
 template <typename T, typename F>
 __device__ __forceinline__ void with_unit(int unit, F&& f) {
-  if (unit >= 8) f(std::integral_constant<int, 8>());
+  if (unit >= 16) f(std::integral_constant<int, 16>());
+  else if (unit == 8) f(std::integral_constant<int, 8>());
   else if (sizeof(T) == 4 || unit == 4) f(std::integral_constant<int, 4>());
   else f(std::integral_constant<int, sizeof(T) == 2 ? 2 : 4>());
 }
 
 // Loads the pieces of a group of G lanes (a power of two up to 32): G * E consecutive values from p on, of which the first
-// n exist (zeros behind them; n may be negative).  ANY: in units below 16 bytes (an instantiation of its own, so that the
+// n exist (zeros behind them; n may be negative).  ANY: exchanged (an instantiation of its own, so that the
 // aligned one is lean).  Whole warps.
 template <bool ANY, typename T>
 __device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G, int lane, int unit, uint8_t* stage) {
@@ -249,11 +255,13 @@ __device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G
       x.load(p + lane * E, unit);
     } else {
       x.clear();
-      if (left > 0) {
-        float v[E];
+      constexpr int kValues = 4 / static_cast<int>(sizeof(T));
+      if (left > 0) {                                        // the row's end, in words
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = i < left ? to_float(p[lane * E + i]) : 0.0f;
-        x.pack(v);
+        for (int i = 0; i < 8; ++i) {
+          if (left >= (i + 1) * kValues) x.w[i] = reinterpret_cast<const uint32_t*>(p + lane * E)[i];
+          else if (kValues == 2 && left == 2 * i + 1) x.w[i] = reinterpret_cast<const unsigned short*>(p + lane * E)[2 * i];
+        }
       }
     }
   } else {
@@ -272,11 +280,12 @@ __device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int 
     if (left >= E) {
       x.store(p + lane * E, unit);
     } else if (left > 0) {
-      float v[E];
-      x.unpack(v);
+      constexpr int kValues = 4 / static_cast<int>(sizeof(T));
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (i < left) p[lane * E + i] = from_float<T>(v[i]);
+      for (int i = 0; i < 8; ++i) {
+        if (left >= (i + 1) * kValues) reinterpret_cast<uint32_t*>(p + lane * E)[i] = x.w[i];
+        else if (kValues == 2 && left == 2 * i + 1) reinterpret_cast<unsigned short*>(p + lane * E)[2 * i] = static_cast<unsigned short>(x.w[i]);
+      }
     }
   } else {
     with_unit<T>(unit, [&](auto u) {

@@ -139,3 +139,28 @@ def test_cache_heads(heads, D, unit, fmt, dtype):
         want[~kept] = 5.0
         assert np.array_equal(out.double().cpu().numpy(), want.reshape(rows, -1))
         assert (around(out, flat) == MARK).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D", [5, 40, 77, 100])
+def test_cache_heads_of_padded_rows(D, fmt, dtype):
+    """Aligned heads whose codes are not."""
+    import torch
+    rng = np.random.default_rng(D)
+    rows, heads = 40, 3
+    k = values(rng, (rows, heads, D), dtype)
+    padded = torch.full((rows, heads, 128), 5.0, dtype=k.dtype, device="cuda")
+    padded[:, :, :D] = k.cuda()
+    cache = binding.QCache.empty(rows, heads, D, FORMATS[fmt])
+    slots = torch.from_numpy(rng.permutation(rows)).cuda()
+    cache.write(slots, padded[:, :, :D], padded[:, :, :D])
+    c, s, want = expect(k.double().numpy(), fmt)
+    for codes, scales in ((cache.k_codes, cache.k_scales), (cache.v_codes, cache.v_scales)):
+        assert np.array_equal(codes[slots].cpu().numpy(), c)
+        assert np.array_equal(scales[slots].cpu().numpy(), s)
+    out = torch.full((2, rows, heads, 128), 7.0, dtype=k.dtype, device="cuda")
+    cache.read(slots, out[0, :, :, :D], out[1, :, :, :D])
+    for got in out:
+        assert np.array_equal(got[:, :, :D].double().cpu().numpy(), want)
+        assert (got[:, :, D:] == 7.0).all()
