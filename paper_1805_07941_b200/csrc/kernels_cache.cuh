@@ -94,7 +94,7 @@ template <int LANES, bool FEW> struct CacheLanes {
 };
 
 // Up to LANES lanes a head, V pieces a lane.  ANY: values or int8 codes that a lane cannot reach by itself go through shared
-// memory, in a part for LANES lanes.
+// memory, in parts for LANES lanes.
 template <typename T, int FMT, int LANES, int V, bool ANY>
 __global__ void __launch_bounds__(kCacheThreads, V == 1 ? kCacheBlocks : 1)
 cache_write_kernel(const CacheArgs a) {
@@ -245,7 +245,7 @@ cache_read_kernel(const CacheArgs a) {
         const float scale = scale_of(sb[j][k]);
         if constexpr (FMT == CACHE_I8 && ANY)
           gather_bytes<E>(w[j][k], raw[j][k], cache_codes(a, c[j]) + k * LANES * E, c[j].valid ? min(a.D - k * LANES * E, LANES * E) : 0, LANES, lane,
-                          stage + (threadIdx.x & 31) / LANES * kStagedBytes<E, LANES>);
+                          stage);
         if constexpr (FMT == CACHE_I8) {
 #pragma unroll
           for (int i = 0; i < E / 4; ++i) i8_decode_four(w[j][k][i], scale, v + 4 * i);

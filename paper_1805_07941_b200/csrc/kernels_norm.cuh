@@ -9,7 +9,7 @@
 // Bound by HBM: x, residual and h once, the codes once.  A row's values stay in registers from the load to the
 // conversion: V pieces of 32 bytes a thread, and as many lanes or warps as that makes for the row's length.  16384 x 8192 bf16
 // with a residual into 4 bits: 134 us, the measured copy rate; rows whose pieces are not aligned pass through shared memory
-// (8192 x 2052 bf16 33.6 us, 2050 39.8, 2049 60.0).
+// (12264 x 2052 bf16 into 4 bits 47 us, 12282 x 2049 65).
 #pragma once
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
@@ -65,9 +65,10 @@ __device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* shared, const 
   return m;
 }
 
-// What a lane has loaded of x and the residual, before it is added up (ANY: dealt pieces).
+// What a lane has loaded of x and the residual, before it is added up (ANY: as the lanes share it out).
 template <typename T> struct NormRaw {
   Piece<T> x, r;
+  uint32_t x_ends, r_ends;                                  // (rows moved by bytes)
 };
 
 // The group's pieces from column `first` on: loaded (all of a thread's loads come before the first use) ...
@@ -77,32 +78,47 @@ __device__ __forceinline__ void norm_fetch(const NormArgs<T>& a, const NormPlace
   const T* px = a.x + at.row * a.ld_x + first;
   const T* pr = a.residual + at.row * a.ld_res + first;
   if constexpr (ANY) {
-    with_unit<T>(a.unit, [&](auto u) {
-      load_dealt<decltype(u)::value>(raw.x, px, n, at.G, at.lane);
-      if (a.residual) load_dealt<decltype(u)::value>(raw.r, pr, n, at.G, at.lane);
-    });
+    if (by_bytes<T>(a.unit)) {
+      load_piece(raw.x, raw.x_ends, px, n, at.G, at.lane);
+      if (a.residual) load_piece(raw.r, raw.r_ends, pr, n, at.G, at.lane);
+    } else {
+      with_unit(a.unit, [&](auto u) {
+        load_dealt<decltype(u)::value>(raw.x, px, n, at.G, at.lane);
+        if (a.residual) load_dealt<decltype(u)::value>(raw.r, pr, n, at.G, at.lane);
+      });
+    }
   } else {
     group_load<false>(raw.x, px, n, at.G, at.lane, a.unit, nullptr);
     if (a.residual) group_load<false>(raw.r, pr, n, at.G, at.lane, a.unit, nullptr);
   }
 }
-// ... and h of them: added, rounded, kept (and then gathered).
-template <bool ANY, typename T>
-__device__ __forceinline__ void norm_add(const NormArgs<T>& a, const NormPlace& at, int first, const NormRaw<T>& raw, Piece<T>& h, uint8_t* stage) {
-  constexpr int E = Piece<T>::E;
-  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
-  h = raw.x;
-  if (a.residual) {
-    float v[E], u[E];
-    raw.x.unpack(v);
-    raw.r.unpack(u);
+template <typename T> __device__ __forceinline__ void add_residual(Piece<T>& h, const Piece<T>& residual) {
+  float v[Piece<T>::E], u[Piece<T>::E];
+  h.unpack(v);
+  residual.unpack(u);
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] += u[i];
-    h.pack(v);                                              // (the rounding to T)
-  }
+  for (int i = 0; i < Piece<T>::E; ++i) v[i] += u[i];
+  h.pack(v);                                                // (the rounding to T)
+}
+// ... and h of them: added, rounded, kept.
+template <bool ANY, typename T>
+__device__ __forceinline__ void norm_add(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T>& raw, Piece<T>& h, uint8_t* stage) {
+  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
   T* ps = a.sum + at.row * a.ld_sum + first;
+  if (ANY && by_bytes<T>(a.unit)) {                         // (the three may begin at different bytes of a word)
+    gather_piece(raw.x, raw.x_ends, a.x + at.row * a.ld_x + first, n, at.G, at.lane, stage);
+    h = raw.x;
+    if (a.residual) {
+      gather_piece(raw.r, raw.r_ends, a.residual + at.row * a.ld_res + first, n, at.G, at.lane, stage);
+      add_residual(h, raw.r);
+    }
+    if (a.sum) store_piece(h, ps, n, at.G, at.lane, stage);
+    return;
+  }
+  h = raw.x;
+  if (a.residual) add_residual(h, raw.r);
   if constexpr (ANY) {
-    with_unit<T>(a.unit, [&](auto u) {
+    with_unit(a.unit, [&](auto u) {
       if (a.sum) store_dealt<decltype(u)::value>(h, ps, n, at.G, at.lane);
       gather_dealt<decltype(u)::value>(h, at.G, at.lane, stage);
     });

@@ -74,7 +74,7 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
 
 // How rows of values may be reached: in units of so many bytes (a power of two from the type's size to 32).  From kLoadUnit
 // on (loads) or kStoreUnit (stores) a lane moves its own values; below, neighbouring lanes take neighbouring units and
-// exchange them through shared memory (group_load).  8192 rows of 4096, 4100, 4098, 4097 bf16 take 16.5, 26.0, 30.0, 35 us to
+// exchange them through shared memory (group_load).  8192 rows of 4096, 4100, 4098, 4097 bf16 take 16.5, 25.3, 29.0, 33.8 us to
 // quantise.  Units of 16 bytes, own and exchanged: 8192 x 4100 float32 quantised in 28.9 and 39.1 us, read back in 41.8 and
 // 35.9; 65536 x 72 bf16 6.3 and 6.2, back 8.9 and 5.6 (two stores a lane, each of parts of sectors).
 constexpr int kLoadUnit = 16, kStoreUnit = 32;
@@ -149,12 +149,81 @@ template <typename T> struct Piece {
   }
 };
 
-// Bytes of shared memory a warp needs for rows that are reached in units below 16 bytes.
-constexpr int kWarpStage = 1024;
+// Bytes from or to p, which may be anywhere, for a group of G lanes (at least four): the first n of G * E.  Neighbouring
+// lanes take neighbouring aligned words, and a few of them the bytes before the first and behind the last word.
+struct ByteRun {
+  int head, words, tail;
+  __device__ __forceinline__ ByteRun(const void* p, int n) {
+    n = max(n, 0);
+    head = min(n, static_cast<int>(-reinterpret_cast<uintptr_t>(p) & 3));
+    words = (n - head) >> 2;
+    tail = (n - head) & 3;
+  }
+};
+// From `bytes`, shared memory (4-byte aligned, readable up to the word behind the last byte's).
+template <int E>
+__device__ __forceinline__ void store_bytes(void* to, const uint8_t* bytes, int n, int G, int lane) {
+  const ByteRun run(to, n);
+  uint8_t* p = static_cast<uint8_t*>(to);
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(bytes);
+  if (lane < run.head) p[lane] = bytes[lane];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) {
+    const int k = i * G + lane;
+    if (k < run.words) *reinterpret_cast<uint32_t*>(p + run.head + 4 * k) = __funnelshift_r(words[k], words[k + 1], 8 * run.head);
+  }
+  const int end = run.head + 4 * run.words + lane;
+  if (lane < run.tail) p[end] = bytes[end];
+}
+// As loaded: a lane's words, and its byte before the first (low) and behind the last.  Then, through the group's part of the
+// warp's shared memory, each lane's own E bytes; where there are none, anything.  Whole warps.
+template <int E> struct DealtBytes {
+  uint32_t w[E / 4], ends;
+};
+template <int E>
+__device__ __forceinline__ void load_bytes(DealtBytes<E>& x, const void* from, int n, int G, int lane) {
+  const ByteRun run(from, n);
+  const uint8_t* p = static_cast<const uint8_t*>(from);
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) x.w[i] = i * G + lane < run.words ? *(reinterpret_cast<const uint32_t*>(p + run.head) + i * G + lane) : 0u;
+  x.ends = lane < run.head ? p[lane] : 0u;
+  if (lane < run.tail) x.ends |= static_cast<uint32_t>(p[run.head + 4 * run.words + lane]) << 8;
+}
+template <int E>
+__device__ __forceinline__ void gather_bytes(uint32_t (&w)[E / 4], const DealtBytes<E>& x, const void* from, int n, int G, int lane, uint8_t* stage) {
+  const ByteRun run(from, n);
+  // byte b at `shift` + b: words stay words, and a lane's bytes begin in its first
+  const int shift = -run.head & 3;
+  uint8_t* group = stage + ((threadIdx.x & 31) - lane) * (E + 4);
+  if (lane < run.head) group[shift + lane] = static_cast<uint8_t>(x.ends);
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i)
+    if (i * G + lane < run.words) reinterpret_cast<uint32_t*>(group + shift + run.head)[i * G + lane] = x.w[i];
+  if (lane < run.tail) group[shift + run.head + 4 * run.words + lane] = static_cast<uint8_t>(x.ends >> 8);
+  __syncwarp();
+  const uint8_t* q = group + lane * E;
+  uint32_t v[E / 4 + 1];
+  if constexpr (E == 8) {
+    const uint2 a = *reinterpret_cast<const uint2*>(q);
+    v[0] = a.x; v[1] = a.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < E / 16; ++i) {
+      const uint4 a = reinterpret_cast<const uint4*>(q)[i];
+      v[4 * i] = a.x; v[4 * i + 1] = a.y; v[4 * i + 2] = a.z; v[4 * i + 3] = a.w;
+    }
+  }
+  v[E / 4] = *reinterpret_cast<const uint32_t*>(q + E);
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 8 * shift);
+  __syncwarp();
+}
+
+// Bytes of shared memory a warp needs to exchange values: 36 a lane (gather_bytes).
+constexpr int kWarpStage = 1152;
 
 // The bits of a unit of U bytes.
-template <int U> struct UnitOf { using type = unsigned short; };
-template <> struct UnitOf<4> { using type = uint32_t; };
+template <int U> struct UnitOf { using type = uint32_t; };
 template <> struct UnitOf<8> { using type = uint2; };
 template <> struct UnitOf<16> { using type = uint4; };
 
@@ -162,14 +231,12 @@ template <> struct UnitOf<16> { using type = uint4; };
 template <int U> __device__ __forceinline__ typename UnitOf<U>::type unit_of(const uint32_t (&w)[8], int i) {
   if constexpr (U == 16) return make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   else if constexpr (U == 8) return make_uint2(w[2 * i], w[2 * i + 1]);
-  else if constexpr (U == 4) return w[i];
-  else return static_cast<unsigned short>(w[i >> 1] >> (16 * (i & 1)));
+  else return w[i];
 }
 template <int U> __device__ __forceinline__ void set_unit(uint32_t (&w)[8], int i, typename UnitOf<U>::type v) {
   if constexpr (U == 16) { w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w; }
   else if constexpr (U == 8) { w[2 * i] = v.x; w[2 * i + 1] = v.y; }
-  else if constexpr (U == 4) w[i] = v;
-  else w[i >> 1] = (i & 1) ? w[i >> 1] | static_cast<uint32_t>(v) << 16 : v;
+  else w[i] = v;
 }
 
 // Dealt pieces from p, where n values exist (zeros behind them), and back; units of U bytes.
@@ -234,13 +301,46 @@ __device__ __forceinline__ void deal(Piece<T>& x, int G, int lane, uint8_t* stag
   for (int i = 0; i < 32 / U; ++i) set_unit<U>(x.w, i, reinterpret_cast<const Unit*>(group)[i * G + lane]);
   __syncwarp();
 }
-// f(the unit as a constant, at most 16 bytes) for a unit that is the same for the whole grid.
-template <typename T, typename F>
-__device__ __forceinline__ void with_unit(int unit, F&& f) {
+// f(the unit as a constant, 4 to 16 bytes) for a unit that is the same for the whole grid.
+template <typename F> __device__ __forceinline__ void with_unit(int unit, F&& f) {
   if (unit >= 16) f(std::integral_constant<int, 16>());
   else if (unit == 8) f(std::integral_constant<int, 8>());
-  else if (sizeof(T) == 4 || unit == 4) f(std::integral_constant<int, 4>());
-  else f(std::integral_constant<int, sizeof(T) == 2 ? 2 : 4>());
+  else f(std::integral_constant<int, 4>());
+}
+// Rows of a 16-bit type that reach 2 bytes alone: by words and, at the ends, bytes; the gathered piece has zeros behind the n
+// values.
+template <typename T> __device__ __forceinline__ bool by_bytes(int unit) { return sizeof(T) == 2 && unit == 2; }
+template <typename T>
+__device__ __forceinline__ int byte_count(int n, int G) { return min(n, G * Piece<T>::E) * static_cast<int>(sizeof(T)); }
+template <typename T>
+__device__ __forceinline__ void load_piece(Piece<T>& x, uint32_t& ends, const T* p, int n, int G, int lane) {
+  DealtBytes<32> dealt;
+  load_bytes<32>(dealt, p, byte_count<T>(n, G), G, lane);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x.w[i] = dealt.w[i];
+  ends = dealt.ends;
+}
+template <typename T>
+__device__ __forceinline__ void gather_piece(Piece<T>& x, uint32_t ends, const T* p, int n, int G, int lane, uint8_t* stage) {
+  DealtBytes<32> dealt;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) dealt.w[i] = x.w[i];
+  dealt.ends = ends;
+  gather_bytes<32>(x.w, dealt, p, byte_count<T>(n, G), G, lane, stage);
+  const int left = n - lane * Piece<T>::E;
+  if (left < Piece<T>::E)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.w[i] = left >= 2 * i + 2 ? x.w[i] : left == 2 * i + 1 ? x.w[i] & 0xFFFFu : 0u;
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(const Piece<T>& x, T* p, int n, int G, int lane, uint8_t* stage) {
+  uint8_t* group = stage + ((threadIdx.x & 31) - lane) * 32;
+  uint4* q = reinterpret_cast<uint4*>(group + lane * 32);
+  q[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+  q[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+  __syncwarp();
+  store_bytes<32>(p, group, byte_count<T>(n, G), G, lane);
+  __syncwarp();
 }
 
 // Loads the pieces of a group of G lanes (a power of two up to 32): G * E consecutive values from p on, of which the first
@@ -265,10 +365,16 @@ __device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G
       }
     }
   } else {
-    with_unit<T>(unit, [&](auto u) {
-      load_dealt<decltype(u)::value>(x, p, n, G, lane);
-      gather_dealt<decltype(u)::value>(x, G, lane, stage);
-    });
+    if (by_bytes<T>(unit)) {
+      uint32_t ends;
+      load_piece(x, ends, p, n, G, lane);
+      gather_piece(x, ends, p, n, G, lane, stage);
+    } else {
+      with_unit(unit, [&](auto u) {
+        load_dealt<decltype(u)::value>(x, p, n, G, lane);
+        gather_dealt<decltype(u)::value>(x, G, lane, stage);
+      });
+    }
   }
 }
 // The same way back: the first n values.
@@ -288,73 +394,16 @@ __device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int 
       }
     }
   } else {
-    with_unit<T>(unit, [&](auto u) {
-      Piece<T> dealt = x;
-      deal<decltype(u)::value>(dealt, G, lane, stage);
-      store_dealt<decltype(u)::value>(dealt, p, n, G, lane);
-    });
+    if (by_bytes<T>(unit)) {
+      store_piece(x, p, n, G, lane, stage);
+    } else {
+      with_unit(unit, [&](auto u) {
+        Piece<T> dealt = x;
+        deal<decltype(u)::value>(dealt, G, lane, stage);
+        store_dealt<decltype(u)::value>(dealt, p, n, G, lane);
+      });
+    }
   }
-}
-
-// Bytes from or to p, which may be anywhere, for a group of G lanes (at least four): the first n of G * E.  Neighbouring
-// lanes take neighbouring aligned words, and a few of them the bytes before the first and behind the last word.
-struct ByteRun {
-  int head, words, tail;
-  __device__ __forceinline__ ByteRun(const uint8_t* p, int n) {
-    n = max(n, 0);
-    head = min(n, static_cast<int>(-reinterpret_cast<uintptr_t>(p) & 3));
-    words = (n - head) >> 2;
-    tail = (n - head) & 3;
-  }
-};
-// From `bytes`, shared memory (4-byte aligned, readable up to the word behind the last byte's).
-template <int E>
-__device__ __forceinline__ void store_bytes(uint8_t* p, const uint8_t* bytes, int n, int G, int lane) {
-  const ByteRun run(p, n);
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(bytes);
-  if (lane < run.head) p[lane] = bytes[lane];
-#pragma unroll
-  for (int i = 0; i < E / 4; ++i) {
-    const int k = i * G + lane;
-    if (k < run.words) *reinterpret_cast<uint32_t*>(p + run.head + 4 * k) = __funnelshift_r(words[k], words[k + 1], 8 * run.head);
-  }
-  const int end = run.head + 4 * run.words + lane;
-  if (lane < run.tail) p[end] = bytes[end];
-}
-
-// As loaded: a lane's words, and its byte before the first (low) and behind the last.  Then, through the group's part of
-// `stage` (kStagedBytes<E, G> of it), each lane's own E bytes; where there are none, anything.  Whole warps.
-template <int E> struct DealtBytes {
-  uint32_t w[E / 4], ends;
-};
-template <int E>
-__device__ __forceinline__ void load_bytes(DealtBytes<E>& x, const uint8_t* p, int n, int G, int lane) {
-  const ByteRun run(p, n);
-#pragma unroll
-  for (int i = 0; i < E / 4; ++i) x.w[i] = i * G + lane < run.words ? __ldg(reinterpret_cast<const uint32_t*>(p + run.head) + i * G + lane) : 0u;
-  x.ends = lane < run.head ? __ldg(p + lane) : 0u;
-  if (lane < run.tail) x.ends |= static_cast<uint32_t>(__ldg(p + run.head + 4 * run.words + lane)) << 8;
-}
-template <int E, int G> constexpr int kStagedBytes = G * E + 8;
-template <int E>
-__device__ __forceinline__ void gather_bytes(uint32_t (&w)[E / 4], const DealtBytes<E>& x, const uint8_t* p, int n, int G, int lane, uint8_t* group) {
-  const ByteRun run(p, n);
-  // byte b is staged at 4 - head + b
-  if (lane < run.head) group[4 - run.head + lane] = static_cast<uint8_t>(x.ends);
-#pragma unroll
-  for (int i = 0; i < E / 4; ++i)
-    if (i * G + lane < run.words) reinterpret_cast<uint32_t*>(group)[1 + i * G + lane] = x.w[i];
-  if (lane < run.tail) group[4 + 4 * run.words + lane] = static_cast<uint8_t>(x.ends >> 8);
-  __syncwarp();
-  const uint32_t* q = reinterpret_cast<const uint32_t*>(group) + ((4 - run.head) >> 2) + lane * (E / 4);
-  uint32_t lo = q[0];
-#pragma unroll
-  for (int i = 0; i < E / 4; ++i) {
-    const uint32_t hi = q[i + 1];
-    w[i] = __funnelshift_r(lo, hi, 8 * ((4 - run.head) & 3));
-    lo = hi;
-  }
-  __syncwarp();
 }
 
 // Bits of the largest |v| over a lane's values, at least infinity's if one is not finite; over the finite ones alone, with
