@@ -489,9 +489,9 @@ int launch_norm(const qc::NormArgs<T>& a, int G, int warps, cudaStream_t st) {
 }
 
 // A row's values in registers: pieces of 32 bytes, one a lane for few rows (the more warps, the shorter the chain of a
-// thread: one row of 4096 bf16 2.5 us, 3.0 with two, 5.6 with four), two for many (16384 x 8192 bf16 into 4 bits 140 us, 189 with
-// one, 154 with four), four where a row is longer than two of every thread hold (unaligned rows only up to two: they pass
-// through registers one by one first).
+// thread: one row of 4096 bf16 2.5 us, 3.0 with two, 5.6 with four), two for many (16384 x 8192 bf16 into 4 bits 140 us, 189
+// with one, 154 with four; 134 since the sums over warps are shorter), four where a row is longer than two of every thread
+// hold (rows that lanes exchange only up to two, which already take 80 registers).
 template <typename T, int OUT>
 int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
   constexpr int E = qc::Piece<T>::E;
