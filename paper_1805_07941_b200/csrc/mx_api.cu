@@ -502,10 +502,11 @@ int run_norm(const qc::NormArgs<T>& a, cudaStream_t st) {
     while (G < lanes) G *= 2;
     return launch_norm<T, OUT, 1>(a, G, 1, st);
   }
-  // Two pieces a thread; one where rows are few, and where an odd number of warps up to three, or five where the rows go
-  // through shared memory, takes one: 16384 x 1536 bf16 to 4 bits 31.1 us against 33.3, 12264 x 2052 48.7 against 59.2;
-  // with seven and eleven warps 7021 x 3584 33.5 against 30.9, 4911 x 5124 54.9 against 51.4.
-  const bool any = a.unit < qc::kLoadUnit, odd = warps(1) % 2 == 1 && warps(1) <= (any ? 5 : 3);
+  // Two pieces a thread; one where rows are few, and where an odd number of warps takes one and the registers still leave
+  // several rows an SM: up to three warps (16384 x 1536 bf16 to 4 bits 31.1 us against 33.3, 7021 x 3584 33.5 against 30.9);
+  // where lanes exchange values, and two pieces take 80 registers, up to nine (5466 x 4604 bf16 40.4 against 48.5, 4911 x 5124
+  // 54.9 against 51.4), or five in float32 (24504 x 1027 72.8 against 80.1, 14794 x 1701 67.3 against 67.2).
+  const bool any = a.unit < qc::kLoadUnit, odd = warps(1) % 2 == 1 && warps(1) <= (!any ? 3 : sizeof(T) == 4 ? 5 : 9);
   if (lanes <= 1024 && (a.rows < 512 || odd)) return launch_norm<T, OUT, 1>(a, 32, warps(1), st);
   if (lanes <= 1024) return launch_norm<T, OUT, 2>(a, 32, warps(2), st);
   if (lanes <= 2048 && !any) return launch_norm<T, OUT, 4>(a, 32, warps(4), st);

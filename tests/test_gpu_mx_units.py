@@ -65,7 +65,7 @@ def test_codec(rows, K, unit, dtype):
 # lengths on either side of the forms: part of a warp, one to nine warps with one piece or two, rows longer than the registers
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("unit", UNITS)
-@pytest.mark.parametrize("rows,C", [(5, 3), (9, 62), (7, 258), (3, 515), (520, 516), (515, 1030), (530, 1542), (3, 2051), (514, 4100), (2, 33001)])
+@pytest.mark.parametrize("rows,C", [(5, 3), (9, 62), (7, 258), (3, 515), (520, 516), (515, 1030), (530, 1542), (3, 2051), (514, 4100), (513, 4612), (513, 5125), (2, 33001)])
 def test_norm(rows, C, unit, dtype):
     import torch
     x, res, gain = make_rows(np.random.default_rng(C + unit), rows, C, dtype)
