@@ -5,6 +5,7 @@
 // way (slot, then codes and scales, are dependent loads).  131072 tokens x 8 heads x 128 bf16, keys and values, int8: written in
 // 146 us (0.85 of the measured copy rate), read back in 135 (0.93).
 #pragma once
+#include "cache_items.cuh"
 #include "mx_format.cuh"
 #include "kernel_igemm.cuh"
 
@@ -39,16 +40,16 @@ struct CacheItem {
   size_t values, group;      // element offset of the head's values; index of (slot, head)
 };
 // The slot of item u (-1 behind the last); items are (row, side, head), head fastest.
-__device__ __forceinline__ long long cache_slot(const CacheArgs& a, int u) {
-  if (u >= a.items) return -1;
+__device__ __forceinline__ long long cache_slot(const CacheArgs& a, unsigned int u) {
+  if (!cache_has(u, a.items)) return -1;
   int h;
-  const int rs = a.fd_heads.divmod(u, &h);
+  const int rs = a.fd_heads.divmod(static_cast<int>(u), &h);
   return __ldg(a.slots + (a.sides == 2 ? rs >> 1 : rs));
 }
-__device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, int u, long long slot) {
+__device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, unsigned int u, long long slot) {
   CacheItem c;
   int h;
-  const int rs = a.fd_heads.divmod(u, &h);
+  const int rs = a.fd_heads.divmod(static_cast<int>(u), &h);
   const int row = a.sides == 2 ? rs >> 1 : rs;
   c.second = a.sides == 2 && (rs & 1);
   c.valid = slot >= 0 && slot < a.num_slots && QC_IN(slot, a.num_slots);
@@ -71,14 +72,14 @@ __device__ __forceinline__ T* cache_values(const CacheArgs& a, const CacheItem& 
 // whole group are idle.  Else LANES each.  (32768 tokens x 8 heads of bf16 to int8, few: 80 values 29.1 us, 96 34.1, 128
 // 38.5; whole: 39.0, 39.4, 39.4.  Back, few: 30.5, 35.6, 40.9; whole: 32.5, 33.9, 36.4, so that reading has it whole.)
 template <int LANES, bool FEW> struct CacheLanes {
-  int G, per_warp, lane, mine;   // mine: which of the warp's heads, past all items where idle
+  int G, per_warp, lane;
+  unsigned int mine;             // which of the warp's heads; past all items where idle
   __device__ __forceinline__ CacheLanes(const CacheArgs& a) {
     const int l = threadIdx.x & 31;
     G = FEW ? a.lanes : LANES;
     per_warp = 32 / G;
-    mine = l / G;
-    lane = l - mine * G;
-    if (FEW && mine >= per_warp) mine = a.items;
+    mine = cache_mine(l, G);
+    lane = l % G;
   }
   // Maximum over a head's lanes: each looks 1, 2, 4, ... lanes ahead, around the group's end.
   __device__ __forceinline__ uint32_t max_over_head(uint32_t m) const {
@@ -103,20 +104,21 @@ cache_write_kernel(const CacheArgs a) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const CacheLanes<LANES, !ANY> at(a);
-  const int lane = at.lane, G = at.G, mine = at.mine, per_block = kCacheThreads / 32 * at.per_warp, step = gridDim.x * per_block;
+  const unsigned int mine = at.mine;
+  const int lane = at.lane, G = at.G, per_block = kCacheThreads / 32 * at.per_warp, step = gridDim.x * per_block;
   uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
   // the lanes of a warp run the same number of rounds
   const int warp_first = (threadIdx.x >> 5) * at.per_warp;
   long long slot[U];
 #pragma unroll
-  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, blockIdx.x * per_block + warp_first + j * step + mine);
+  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, cache_unit(blockIdx.x * per_block + warp_first + j * step, mine));
   for (int base = blockIdx.x * per_block + warp_first; base < a.items; base += U * step) {
     CacheItem c[U];
     Piece<T> x[U][V];
 #pragma unroll
-    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine, slot[j]);
+    for (int j = 0; j < U; ++j) c[j] = cache_item(a, cache_unit(base + j * step, mine), slot[j]);
 #pragma unroll
-    for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, base + (U + j) * step + mine);
+    for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, cache_unit(base + (U + j) * step, mine));
 #pragma unroll
     for (int j = 0; j < U; ++j)
 #pragma unroll
@@ -183,18 +185,19 @@ cache_read_kernel(const CacheArgs a) {
   const int lane = threadIdx.x & (LANES - 1);
   const int step = gridDim.x * kPerBlock;
   uint8_t* stage = stages[ANY ? threadIdx.x >> 5 : 0];
-  const int warp_first = (threadIdx.x >> 5) * kPerWarp, mine = (threadIdx.x & 31) / LANES;
+  const int warp_first = (threadIdx.x >> 5) * kPerWarp;
+  const unsigned int mine = cache_mine(threadIdx.x & 31, LANES);
   long long slot[U];
 #pragma unroll
-  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, blockIdx.x * kPerBlock + warp_first + j * step + mine);
+  for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, cache_unit(blockIdx.x * kPerBlock + warp_first + j * step, mine));
   for (int base = blockIdx.x * kPerBlock + warp_first; base < a.items; base += U * step) {
     CacheItem c[U];
     uint32_t w[U][V][E / 4], sb[U][V];                      // (4-bit codes: the first half)
     DealtBytes<E> raw[FMT == CACHE_I8 && ANY ? U : 1][V];
 #pragma unroll
-    for (int j = 0; j < U; ++j) c[j] = cache_item(a, base + j * step + mine, slot[j]);
+    for (int j = 0; j < U; ++j) c[j] = cache_item(a, cache_unit(base + j * step, mine), slot[j]);
 #pragma unroll
-    for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, base + (U + j) * step + mine);
+    for (int j = 0; j < U; ++j) slot[j] = cache_slot(a, cache_unit(base + (U + j) * step, mine));
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const uint8_t* codes = cache_codes(a, c[j]);
