@@ -16,7 +16,8 @@
 // Warp roles (320 threads): warp 0 issues TMA loads, warp 1 owns tensor memory and issues
 // the MMAs, warps 2-9 run the epilogue (each reads the TMEM lane quadrant warp_id % 4 and one
 // half of the tile's columns).
-// All waits on mbarriers are bounded; on expiry the CTA raises a status flag and leaves.
+// All waits on mbarriers are bounded; on expiry the CTA raises a status flag and leaves.  (Why the allocation of tensor memory
+// and, where CTAs share a tile, their cluster's barriers end: tensor_memory.cuh.)
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>

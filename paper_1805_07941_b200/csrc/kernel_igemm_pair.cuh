@@ -11,8 +11,8 @@
 // Barriers: a stage's "full" barrier lives in the first CTA and counts the bytes of both CTAs' loads (the
 // second CTA's copies signal it across the cluster); "empty" and "accumulator full" are signalled in both
 // CTAs at once by the MMA thread's multicast commits; "accumulator empty" lives in the first CTA and is
-// arrived on by the epilogue warps of both.  All waits are bounded; the two CTAs meet at a cluster barrier
-// before any remote signal and before they retire.
+// arrived on by the epilogue warps of both.  All waits on them are bounded; the two CTAs meet at a cluster barrier
+// before any remote signal and before they retire (why it, and the allocation of tensor memory, end: tensor_memory.cuh).
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>

@@ -16,7 +16,8 @@
 // Roles (128 threads): warp 0 issues the loads, warp 1 owns tensor memory and issues copies and MMAs, then all four warps
 // drain a quarter of the lanes each.  With few tiles a cluster of CTAs shares a tile: each takes a part of the contraction
 // and sends its sums to the CTAs' shared memory, a share of the columns each, where they are added up in a fixed order (no
-// scratch in global memory, and the same result each time).  All waits are bounded.
+// scratch in global memory, and the same result each time).  All waits on mbarriers are bounded; why the cluster's own barriers
+// and the allocation of tensor memory end is in tensor_memory.cuh.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>

@@ -18,7 +18,8 @@
 // Roles per CTA (320 threads): warp 0 lane 0 issues the loads, warp 1 owns tensor memory (lane 0 of the first CTA issues
 // scale copies and MMAs for both), warps 2-9 are the epilogue: tensor-memory lanes warp % 4, one half of the columns each.
 // Barriers as in kernel_igemm_pair.cuh: a stage's "full" lives in the first CTA and counts both CTAs' bytes; "empty" and
-// "accumulator full" arrive in both by multicast commits; "accumulator free" lives in the first CTA.  All waits are bounded.
+// "accumulator full" arrive in both by multicast commits; "accumulator free" lives in the first CTA.  All waits on them are bounded;
+// why the cluster's own barriers and the allocation of tensor memory end is in tensor_memory.cuh.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -31,11 +32,12 @@ namespace qc {
 constexpr int kMxPairThreads = 64 + 32 * 8;
 constexpr int kMxPairStages = 5;
 constexpr int kMxPairTokens = 192;                                       // columns of a tile
+constexpr int kMxPairCols = 512;                                         // of tensor memory
 constexpr uint32_t kMxPairA = 128 * kMxStageBytes, kMxPairB = kMxPairTokens / 2 * kMxStageBytes;
 constexpr uint32_t kMxPairScaleB = 4 * kMxTileBytes;                     // of the 256 tokens whose scale tiles a tile touches
 constexpr uint32_t kMxPairStage = kMxPairA + kMxPairB + 2 * kMxTileBytes + kMxPairScaleB;
 constexpr int kMxPairScaleCol = 2 * kMxPairTokens, kMxPairScaleCols = 24;
-static_assert(kMxPairScaleCol + kMxPairStages * kMxPairScaleCols <= 512 && kMxPairStage % 1024 == 0);
+static_assert(kMxPairScaleCol + kMxPairStages * kMxPairScaleCols <= kMxPairCols && kMxPairStage % 1024 == 0);
 
 struct MxPairShared {
   uint64_t full[kMxPairStages];
@@ -191,7 +193,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     ptx::prefetch_tmap(&map_xs);
   }
   if (warp == 1) {
-    ptx::tmem_alloc_pair(ptx::smem_u32(&sh->tmem_base), 512);
+    ptx::tmem_alloc_pair(ptx::smem_u32(&sh->tmem_base), kMxPairCols);
     ptx::tmem_relinquish_pair();
   }
   ptx::tc_fence_before();
@@ -358,7 +360,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
   ptx::cluster_sync_all();
   if (warp == 1) {
     ptx::tc_fence_after();
-    ptx::tmem_dealloc_pair(tmem, 512);
+    ptx::tmem_dealloc_pair(tmem, kMxPairCols);
   }
 }
 

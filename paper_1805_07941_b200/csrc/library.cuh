@@ -13,6 +13,7 @@
 
 #include "../../include/qconv.h"
 #include "kernel_igemm.cuh"
+#include "tensor_memory.cuh"
 
 #define QC_HIDDEN __attribute__((visibility("hidden")))
 
@@ -63,6 +64,26 @@ cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, dim3 block, size
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// Launch in clusters of CTAs that allocate `columns` columns of tensor memory each; `chained` as above.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned int grid, unsigned int cluster, unsigned int threads, size_t smem, int columns,
+                            bool chained, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = cluster_smem(smem, columns);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = chained ? 1 : 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 inline int grid_for(size_t work_items, int threads, int max_blocks) {

@@ -221,6 +221,8 @@ struct qmx_linear {
   int device = 0, num_sms = 148;
   CUtensorMap map_w, map_ws;
   int bn = 0, split = 0, stages = 0;     // the last run's form
+  int columns = 0;                       // of tensor memory, and bytes of shared memory of a CTA
+  size_t smem = 0;
   bool pair = false, staged = false;
   unsigned int wait_limit = 1u << 22;
   cudaStream_t last_stream = nullptr;
@@ -282,50 +284,35 @@ int launch_gemm(qmx_linear* h, const MxRunMaps& maps, qc::MxGemmParams prm, Y* y
   const uint32_t room = (alone ? 227u : 113u) * 1024 - 1024 - sizeof(qc::MxGemmShared) - sums;
   prm.stages = std::max(2, std::min({per_cta, static_cast<int>(room / Tile::kStage), Tile::kMaxStages}));
   const size_t smem = 1024 + static_cast<size_t>(prm.stages) * Tile::kStage + sizeof(qc::MxGemmShared) + sums;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned int>(prm.tiles_n) * prm.tiles_t * prm.split);
-  cfg.blockDim = dim3(qc::kMxGemmThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = qc::chained_launches() ? 1 : 0;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = prm.split;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = prm.split > 1 ? 2 : 1;
+  const unsigned int grid = static_cast<unsigned int>(prm.tiles_n) * prm.tiles_t * prm.split;
+  const auto kernel = qc::mx_gemm_kernel<BN, Y>;
   h->bn = BN; h->split = prm.split; h->stages = prm.stages; h->pair = h->staged = false;
-  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_kernel<BN, Y>, h->map_w, maps.x, h->map_ws, maps.xs, prm, h->bias, y, h->d_status,
-                              h->wait_limit));
+  h->columns = Tile::kCols; h->smem = prm.split > 1 ? qc::cluster_smem(smem, Tile::kCols) : smem;
+  if (prm.split > 1)
+    CUDA_TRY(qc::launch_clusters(kernel, grid, prm.split, qc::kMxGemmThreads, smem, Tile::kCols, qc::chained_launches(), st, h->map_w, maps.x,
+                                 h->map_ws, maps.xs, prm, h->bias, y, h->d_status, h->wait_limit));
+  else
+    CUDA_TRY(launch_chained(kernel, dim3(grid), dim3(qc::kMxGemmThreads), smem, st, h->map_w, maps.x, h->map_ws, maps.xs, prm, h->bias, y,
+                            h->d_status, h->wait_limit));
   return QCONV_OK;
 }
 
 template <typename Y, bool STAGED>
 cudaError_t allow_pair_smem() {
-  return cudaFuncSetAttribute(qc::mx_gemm_pair_kernel<Y, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (qc::kMxPairSmem<Y, STAGED>));
+  return cudaFuncSetAttribute(qc::mx_gemm_pair_kernel<Y, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
 }
 
 template <typename Y, bool STAGED>
 int launch_pair(qmx_linear* h, const MxRunMaps& maps, qc::MxGemmParams prm, Y* y, cudaStream_t st) {
   static qc::PerDevice<cudaError_t> allowed;
   CUDA_TRY(allowed.once(h->device, allow_pair_smem<Y, STAGED>));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2u * std::min(prm.tiles_n * prm.tiles_t, h->num_sms / 2));
-  cfg.blockDim = dim3(qc::kMxPairThreads);
-  cfg.dynamicSmemBytes = (qc::kMxPairSmem<Y, STAGED>);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = qc::chained_launches() ? 1 : 0;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  const unsigned int grid = 2u * std::min(prm.tiles_n * prm.tiles_t, h->num_sms / 2);
+  const size_t smem = qc::kMxPairSmem<Y, STAGED>;
+  const auto kernel = qc::mx_gemm_pair_kernel<Y, STAGED>;
   h->bn = qc::kMxPairTokens; h->split = 1; h->stages = qc::kMxPairStages; h->pair = true; h->staged = STAGED;
-  CUDA_TRY(cudaLaunchKernelEx(&cfg, qc::mx_gemm_pair_kernel<Y, STAGED>, h->map_w, maps.x, h->map_ws, maps.xs, maps.y, prm, h->bias, y,
-                              h->d_status, h->wait_limit));
+  h->columns = qc::kMxPairCols; h->smem = qc::cluster_smem(smem, qc::kMxPairCols);
+  CUDA_TRY(qc::launch_clusters(kernel, grid, 2, qc::kMxPairThreads, smem, qc::kMxPairCols, qc::chained_launches(), st, h->map_w, maps.x,
+                               h->map_ws, maps.xs, maps.y, prm, h->bias, y, h->d_status, h->wait_limit));
   return QCONV_OK;
 }
 
@@ -448,8 +435,8 @@ int qmx_linear_set_wait_limit(qmx_linear* h, unsigned int polls) {
 
 int qmx_linear_describe(const qmx_linear* h, char* buf, size_t buf_len) {
   if (!h || !buf || buf_len == 0) return fail(QCONV_ERR_BAD_ARG, "NULL argument");
-  snprintf(buf, buf_len, "mx N=%d K=%d tile=%dx%d split=%d pair=%d stages=%d staged=%d", h->d.N, h->d.K, h->pair ? 256 : 128, h->bn, h->split,
-           h->pair, h->stages, h->staged);
+  snprintf(buf, buf_len, "mx N=%d K=%d tile=%dx%d split=%d pair=%d stages=%d staged=%d smem=%zu columns=%d", h->d.N, h->d.K, h->pair ? 256 : 128, h->bn, h->split,
+           h->pair, h->stages, h->staged, h->smem, h->columns);
   return QCONV_OK;
 }
 

@@ -863,6 +863,7 @@ int plan_igemm(qconv_handle* h, DeviceParts& parts, const qconv_handle* weights_
   h->smem_bytes = 1024 + static_cast<size_t>(stages) * (p.a_stage_bytes + (p.b_resident ? 0 : p.b_stage_bytes)) +
                   (p.b_resident ? static_cast<size_t>(num_kb_plan) * p.b_stage_bytes : 0) +
                   static_cast<size_t>(staged_tiles) * p.out_stage_bytes + p.gen_stage_bytes + sizeof(qc::IgemmShared);
+  if (h->pair) h->smem_bytes = qc::cluster_smem(h->smem_bytes, 2 * p.tmem_cols);
   p.stride_h = p.stride_w = 1;
   p.pad_h = p.pad_w = 0;
   if (h->mode == MODE_FLAT || h->mode == MODE_STEM) {
@@ -1976,21 +1977,10 @@ int run_layer(qconv_handle* h, const int8_t* d_x, const int8_t* d_residual, void
       const long pair_tiles = static_cast<long>(pp.pairs_m) * pp.tiles_k;
       if (pair_tiles <= 0 || pair_tiles > 1073741823l) return fail(QCONV_ERR_UNSUPPORTED_SHAPE, "tile count out of range");
       const long pairs = std::min<long>(pair_tiles, h->num_sms / 2);
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(static_cast<unsigned int>(2 * pairs));
-      cfg.blockDim = dim3(qc::kIgemmThreads);
-      cfg.dynamicSmemBytes = h->smem_bytes;
-      cfg.stream = st;
-      cudaLaunchAttribute attr[2];
-      attr[0].id = cudaLaunchAttributeClusterDimension;
-      attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-      attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      attr[1].val.programmaticStreamSerializationAllowed = h->use_pdl;
-      cfg.attrs = attr;
-      cfg.numAttrs = 2;
       const int4* chan_ptr = h->d_chan;
-      cudaError_t le = cudaLaunchKernelEx(&cfg, pair_kernel_for(h), h->tmap_a, h->tmap_b, pp, p, ep, chan_ptr, d_y,
-                                          h->d_status, h->wait_limit);
+      cudaError_t le = qc::launch_clusters(pair_kernel_for(h), static_cast<unsigned int>(2 * pairs), 2, qc::kIgemmThreads, h->smem_bytes,
+                                           2 * pp.tmem_cols, h->use_pdl != 0, st, h->tmap_a, h->tmap_b, pp, p, ep, chan_ptr, d_y, h->d_status,
+                                           h->wait_limit);
       if (le != cudaSuccess) return fail(QCONV_ERR_CUDA, "kernel launch (SM pairs): %s", cudaGetErrorString(le));
       return QCONV_OK;
     }
@@ -2000,24 +1990,14 @@ int run_layer(qconv_handle* h, const int8_t* d_x, const int8_t* d_residual, void
       const int num_kb = p.R * p.S * p.nchunks, own = p.BN / 16 / ksplit;
       q.ksplit = ksplit;
       q.out_stage_bytes = 0;
+      q.acc_bufs = 1;                                        // (a CTA has one tile)
       q.gen_stage_bytes = static_cast<uint32_t>(own * (ksplit - 1) * 4 * 128 * 16);       // exchange area
       const size_t fixed = 1024 + q.gen_stage_bytes + sizeof(qc::IgemmShared), stage = p.a_stage_bytes + p.b_stage_bytes;
       q.stages = std::min<int>({ceil_div(num_kb, ksplit), qc::kMaxStages, static_cast<int>((226 * 1024 - fixed) / stage)});
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(static_cast<unsigned int>(tiles * ksplit));
-      cfg.blockDim = dim3(qc::kIgemmThreads);
-      cfg.dynamicSmemBytes = fixed + q.stages * stage;
-      cfg.stream = st;
-      cudaLaunchAttribute attr[2];
-      attr[0].id = cudaLaunchAttributeClusterDimension;
-      attr[0].val.clusterDim.x = static_cast<unsigned int>(ksplit); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-      attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      attr[1].val.programmaticStreamSerializationAllowed = h->use_pdl;
-      cfg.attrs = attr;
-      cfg.numAttrs = 2;
       const int4* chan_ptr = h->d_chan;
-      cudaError_t le = cudaLaunchKernelEx(&cfg, split_kernel_for(h), h->tmap_a, h->tmap_b, h->tmap_a, h->tmap_a, q, ep, chan_ptr, d_residual,
-                                          d_y, h->d_status, h->wait_limit);
+      cudaError_t le = qc::launch_clusters(split_kernel_for(h), static_cast<unsigned int>(tiles * ksplit), static_cast<unsigned int>(ksplit),
+                                           qc::kIgemmThreads, fixed + q.stages * stage, q.tmem_cols, h->use_pdl != 0, st, h->tmap_a, h->tmap_b,
+                                           h->tmap_a, h->tmap_a, q, ep, chan_ptr, d_residual, d_y, h->d_status, h->wait_limit);
       if (le != cudaSuccess) return fail(QCONV_ERR_CUDA, "kernel launch (split contraction): %s", cudaGetErrorString(le));
       return QCONV_OK;
     }
