@@ -22,13 +22,10 @@ namespace qc {
 // Keeps the text for qconv_last_error_string (of the calling thread) and returns `code`.
 QC_HIDDEN int fail(int code, const char* fmt, ...);
 
-// cuTensorMapEncodeTiled is resolved through the runtime so the library links only cudart.
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-QC_HIDDEN EncodeTiledFn get_encode_fn();
+// Tensor map of `base`, not interleaved, zeros outside; QCONV_OK or an error with its text.  From any host thread.
+QC_HIDDEN int encode_tiled(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims,
+                           const cuuint64_t* strides_bytes, const cuuint32_t* box, const cuuint32_t* elem_strides, CUtensorMapSwizzle swizzle,
+                           CUtensorMapL2promotion promotion);
 
 // Whether the calling thread's plan hints leave programmatic dependent launch on.
 QC_HIDDEN bool chained_launches();

@@ -241,14 +241,9 @@ namespace {
 
 int encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, cuuint64_t inner, cuuint64_t rows, cuuint64_t pitch,
               cuuint32_t box_inner, cuuint32_t box_rows, CUtensorMapSwizzle swizzle) {
-  const qc::EncodeTiledFn fn = qc::get_encode_fn();
-  if (!fn) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   const cuuint64_t dims[2] = {inner, rows}, strides[1] = {pitch};
   const cuuint32_t box[2] = {box_inner, box_rows}, steps[2] = {1, 1};
-  const CUresult r = fn(map, type, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
-  return QCONV_OK;
+  return qc::encode_tiled(map, type, 2, base, dims, strides, box, steps, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 // Codes [rows][K] in boxes of `box_rows` rows x 256 values, and their scale tiles in boxes of two tiles along the
 // contraction x those of `scale_rows` rows (what a box reaches beyond the arrays is read as zeros).

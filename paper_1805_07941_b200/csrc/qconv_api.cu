@@ -36,11 +36,9 @@
 static_assert(QCALIB_STATIC_MAX_BINS <= qc::kCalibMaxBins, "built-in scratch holds kCalibMaxBins counters");
 
 using qc::fail;
-using qc::get_encode_fn;
 using qc::grid_for;
 using qc::launch_chained;
 using qc::make_fastdiv;
-using qc::EncodeTiledFn;
 
 namespace {
 
@@ -55,15 +53,10 @@ CUtensorMapSwizzle swizzle_for(int bkc) {
 int encode_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims,
                const cuuint64_t* strides_bytes /* rank-1 */, const cuuint32_t* box, int bkc,
                const cuuint32_t* elem_strides = nullptr) {
-  EncodeTiledFn fn = get_encode_fn();
-  if (!fn) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   for (int i = 0; i < rank && elem_strides; ++i) estr[i] = elem_strides[i];
-  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, static_cast<cuuint32_t>(rank), const_cast<void*>(base),
-                  dims, strides_bytes, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle_for(bkc),
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
-  return QCONV_OK;
+  return qc::encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, base, dims, strides_bytes, box, estr, swizzle_for(bkc),
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -90,7 +83,13 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-EncodeTiledFn get_encode_fn() {
+// cuTensorMapEncodeTiled is resolved through the runtime so the library links only cudart.
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+
+static EncodeTiledFn get_encode_fn() {
   static EncodeTiledFn fn = nullptr;
   static std::once_flag once;
   std::call_once(once, [] {
@@ -101,6 +100,25 @@ EncodeTiledFn get_encode_fn() {
       fn = reinterpret_cast<EncodeTiledFn>(p);
   });
   return fn;
+}
+
+int encode_tiled(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides_bytes,
+                 const cuuint32_t* box, const cuuint32_t* elem_strides, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion) {
+  const EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+  const auto encode = [&] {
+    return fn(map, type, static_cast<cuuint32_t>(rank), const_cast<void*>(base), dims, strides_bytes, box, elem_strides,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  };
+  CUresult r = encode();
+  if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+    // A host thread has no current context before its first call that needs one, and this one, of the driver's, makes none
+    // (cudaGetDevice does not either; cudaSetDevice does).
+    int dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) r = encode();
+  }
+  if (r != CUDA_SUCCESS) return fail(QCONV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
+  return QCONV_OK;
 }
 
 bool chained_launches() { return g_hints.pdl != 0; }
