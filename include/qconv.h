@@ -470,8 +470,10 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
  *                           and must outlive the handle; a run reads what they hold then.
  * A handle belongs to the device that is current when it is made (not while a stream is being captured); running it elsewhere
  * is BAD_ARG.  It holds no scratch: runs may overlap on several streams, but one host thread uses it at a time.  Dropping it
- * waits for the device.  Device-side waits are bounded as
- * qconv_run's are; qmx_linear_status synchronises the stream of the last run and returns (and clears) the device status,
+ * waits for the device, so it is not dropped while a stream is being captured; and it must outlive the graphs that its runs
+ * were captured into, which hold the address of its status word.  Device-side waits are bounded as
+ * qconv_run's are; qmx_linear_status synchronises the stream of the last run (a replay's stream is the caller's to
+ * synchronise first) and returns (and clears) the device status,
  * qmx_linear_set_wait_limit is the test hook that qconv_set_wait_limit is. */
 typedef struct {
   int N, K;

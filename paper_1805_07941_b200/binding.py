@@ -762,7 +762,8 @@ def qmx_dequantize(codes, scales, K, layout=MX_TILES, dtype=None, out=None):
 
 class QMXLinear:
     """An inner-product layer on microscaled 4-bit operands (qmx_linear_create / run / status / destroy): weights as
-    qmx_quantize(w [N, K], layout=MX_TILES) gives them, kept by this object and read where they lie."""
+    qmx_quantize(w [N, K], layout=MX_TILES) gives them, kept by this object and read where they lie.  It must outlive the graphs
+    that its runs were captured into, and is not dropped during a capture."""
 
     def __init__(self, w_codes, w_scales, N, K, bias=None, relu=0, dtype=None):
         import torch

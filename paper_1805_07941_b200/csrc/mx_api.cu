@@ -17,6 +17,7 @@
 #include "kernels_norm.cuh"
 #include "library.cuh"
 #include "per_device.cuh"
+#include "status_words.cuh"
 
 // The header's numbers and the kernels'.
 constexpr int kOfHeader[] = {QTYPE_F32, QTYPE_BF16, QTYPE_F16, QNORM_I8, QNORM_I8_ROWS, QNORM_MX, QCACHE_I8, QCACHE_MX};
@@ -177,46 +178,15 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
 // --------------------------------------------------------------------------- products
 }  // extern "C"
 
-// The handles' status words: up to 1024 a device out of one allocation that stays (4 KB), so that making and dropping a handle
-// costs no cudaMalloc and cudaFree (13 us instead of 0.8 ms where it is the device's only one); more come from the pool.
-class StatusWords {
- public:
-  static StatusWords& words() {
-    static StatusWords* w = new StatusWords;               // never destroyed, as the pool
-    return *w;
-  }
-  cudaError_t take(int device, int** word) {
-    std::lock_guard<std::mutex> lock(mu_);
-    PerDevice& d = per_device_[device & 63];
-    if (!d.base) {
-      const cudaError_t e = DevicePool::pool().plain(&d.base, kWords * sizeof(int));
-      if (e != cudaSuccess) { d.base = nullptr; return e; }
-    }
-    *word = nullptr;
-    for (int i = 0; i < kWords && !*word; ++i)
-      if (!d.used[i]) { d.used[i] = true; *word = d.base + i; }
-    return cudaSuccess;
-  }
-  void give(int device, int* word) {
-    std::lock_guard<std::mutex> lock(mu_);
-    PerDevice& d = per_device_[device & 63];
-    d.used[word - d.base] = false;
-  }
-
- private:
-  static constexpr int kWords = 1024;
-  struct PerDevice {
-    int* base = nullptr;
-    bool used[kWords] = {};
-  };
-  std::mutex mu_;
-  PerDevice per_device_[64];
-};
+static qc::StatusWords& status_words() {
+  static qc::StatusWords* w = new qc::StatusWords;         // never destroyed, as the pool
+  return *w;
+}
 
 struct qmx_linear {
   qmx_linear_desc d;
   const float* bias;
-  DevicePool::Block block;               // of the status word where StatusWords has none left
+  DevicePool::Block block;               // of the status word where status_words() has none left
   int* d_status = nullptr;
   int device = 0, num_sms = 148;
   CUtensorMap map_w, map_ws;
@@ -230,10 +200,11 @@ struct qmx_linear {
     if (!d_status || block.ptr) return;
     // (whoever takes the word next must not see a status of this handle's)
     int dev = 0;
-    const bool other = cudaGetDevice(&dev) == cudaSuccess && dev != device && cudaSetDevice(device) == cudaSuccess;
-    cudaDeviceSynchronize();
-    if (other) cudaSetDevice(dev);
-    StatusWords::words().give(device, d_status);
+    const bool known = cudaGetDevice(&dev) == cudaSuccess, here = known && (dev == device || cudaSetDevice(device) == cudaSuccess);
+    const bool idle = here && cudaDeviceSynchronize() == cudaSuccess;
+    if (here && dev != device) cudaSetDevice(dev);
+    if (!idle) cudaGetLastError();                         // (no later call's)
+    status_words().give(device, d_status, idle);
   }
 };
 
@@ -331,7 +302,7 @@ int qmx_linear_create(qmx_linear** out, const qmx_linear_desc* desc, const uint8
   rc = encode_operand(&h->map_w, &h->map_ws, d_w_codes, d_w_scales, desc->N, desc->K, 128, 128);
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
-  if (!rc && e == cudaSuccess) e = StatusWords::words().take(h->device, &h->d_status);
+  if (!rc && e == cudaSuccess) e = status_words().take(h->device, &h->d_status, [](int** base, size_t bytes) { return DevicePool::pool().plain(base, bytes); });
   if (!rc && e == cudaSuccess && !h->d_status) {
     e = DevicePool::pool().take(&h->block, sizeof(int));
     h->d_status = static_cast<int*>(h->block.ptr);
