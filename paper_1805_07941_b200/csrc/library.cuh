@@ -83,6 +83,22 @@ cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned int grid, unsigne
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Another device for a while: current from here to the end of the scope where `there`.
+class DeviceScope {
+ public:
+  explicit DeviceScope(int device) {
+    there = cudaGetDevice(&before_) == cudaSuccess && (before_ == device || (other_ = cudaSetDevice(device) == cudaSuccess));
+  }
+  ~DeviceScope() { if (other_) cudaSetDevice(before_); }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+  bool there = false;
+
+ private:
+  int before_ = 0;
+  bool other_ = false;
+};
+
 inline int grid_for(size_t work_items, int threads, int max_blocks) {
   size_t b = (work_items + threads - 1) / threads;
   return static_cast<int>(std::max<size_t>(1, std::min<size_t>(b, max_blocks)));

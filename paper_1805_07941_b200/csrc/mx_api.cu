@@ -199,10 +199,8 @@ struct qmx_linear {
   ~qmx_linear() {
     if (!d_status || block.ptr) return;
     // (whoever takes the word next must not see a status of this handle's)
-    int dev = 0;
-    const bool known = cudaGetDevice(&dev) == cudaSuccess, here = known && (dev == device || cudaSetDevice(device) == cudaSuccess);
-    const bool idle = here && cudaDeviceSynchronize() == cudaSuccess;
-    if (here && dev != device) cudaSetDevice(dev);
+    const qc::DeviceScope at(device);
+    const bool idle = at.there && cudaDeviceSynchronize() == cudaSuccess;
     if (!idle) cudaGetLastError();                         // (no later call's)
     status_words().give(device, d_status, idle);
   }
@@ -383,6 +381,8 @@ int qmx_linear_run(qmx_linear* h, const uint8_t* d_x_codes, const uint8_t* d_x_s
 
 int qmx_linear_status(qmx_linear* h) {
   if (!h) return fail(QCONV_ERR_BAD_ARG, "NULL handle");
+  const qc::DeviceScope at(h->device);                     // (the default stream is the current device's)
+  if (!at.there) return fail(QCONV_ERR_CUDA, "qmx_linear_status: cannot make device %d current", h->device);
   CUDA_TRY(cudaStreamSynchronize(h->last_stream));
   int st = 0;
   CUDA_TRY(cudaMemcpy(&st, h->d_status, sizeof(int), cudaMemcpyDeviceToHost));

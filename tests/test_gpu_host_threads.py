@@ -112,6 +112,28 @@ def test_the_other_operators_first_calls():
     assert torch.equal(values, cached())
 
 
+def test_a_status_is_waited_for_on_the_handles_device():
+    """From another device: the default stream that is waited for is the one of the handle's."""
+    import torch
+    if torch.cuda.device_count() < 2:
+        pytest.skip("needs two devices")
+    T, N, K = 8192, 8192, 8192
+    wc, ws, xc, xs, want = product(T, N, K)
+    lin = binding.QMXLinear(wc, ws, N, K, dtype=torch.float32)
+    y = torch.empty_like(want)
+    for _ in range(20):
+        lin.run(xc, xs, y)
+    after = torch.cuda.Event()
+    after.record()
+    with torch.cuda.device(1):
+        assert lin.status() == 0 and after.query()
+        assert torch.cuda.current_device() == 1
+        with pytest.raises(ValueError):
+            lin.run(xc, xs, y)
+        lin.destroy()
+        assert torch.cuda.current_device() == 1
+
+
 def test_an_int8_layer_in_a_thread():
     """Made and run there; and a layer made here that first runs there, on an input that it has no tensor map of."""
     import torch
