@@ -546,7 +546,7 @@ int qcache_read(const qcache_desc* cache, const int64_t* d_slots, long long rows
                 const qcache_values* values, int type, void* cuda_stream);
 
 /* Checked build of the library (compiled with -DQCONV_CHECKED, binding.build_library(checked=True)): in the
- * CUDA-core kernels (conversions, pooling, packing, depthwise / direct convolution, eltwise, digit planes) every
+ * CUDA-core kernels (conversions, pooling, packing, depthwise / direct convolution, eltwise, digit planes, microscaled codec, norm, caches) every
  * global access with a computed address first tests its index against the tensor's extent; a failing test is
  * counted, the access skipped, the kernel goes on.  Returns the number of failed tests since the last call (and
  * the source line of the first in *first_line_out), clearing it; synchronises the device.  A normal build

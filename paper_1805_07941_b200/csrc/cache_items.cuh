@@ -3,11 +3,7 @@
 // item of a round lies at most a few steps of the grid (148 * 8 blocks of up to 64 heads) behind the last, so that unsigned sums
 // stay below 2^31 + 2^20.  (Signed, those of idle lanes would turn negative in lists of nearly 2^30 items.)
 #pragma once
-#ifdef __CUDACC__
-#define QC_ANY_SIDE __host__ __device__ __forceinline__
-#else
-#define QC_ANY_SIDE inline
-#endif
+#include "any_side.cuh"
 
 namespace qc {
 

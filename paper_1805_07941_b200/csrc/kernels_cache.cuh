@@ -39,12 +39,13 @@ struct CacheItem {
   bool valid, second;        // second: of the values, not the keys
   size_t values, group;      // element offset of the head's values; index of (slot, head)
 };
+__device__ __forceinline__ int cache_rows(const CacheArgs& a) { return a.items / (a.heads * a.sides); }
 // The slot of item u (-1 behind the last); items are (row, side, head), head fastest.
 __device__ __forceinline__ long long cache_slot(const CacheArgs& a, unsigned int u) {
   if (!cache_has(u, a.items)) return -1;
   int h;
-  const int rs = a.fd_heads.divmod(static_cast<int>(u), &h);
-  return __ldg(a.slots + (a.sides == 2 ? rs >> 1 : rs));
+  const int rs = a.fd_heads.divmod(static_cast<int>(u), &h), row = a.sides == 2 ? rs >> 1 : rs;
+  return QC_IN(row, cache_rows(a)) ? __ldg(a.slots + row) : -1;
 }
 __device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, unsigned int u, long long slot) {
   CacheItem c;
@@ -52,7 +53,7 @@ __device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, unsigned int
   const int rs = a.fd_heads.divmod(static_cast<int>(u), &h);
   const int row = a.sides == 2 ? rs >> 1 : rs;
   c.second = a.sides == 2 && (rs & 1);
-  c.valid = slot >= 0 && slot < a.num_slots && QC_IN(slot, a.num_slots);
+  c.valid = slot >= 0 && slot < a.num_slots;
   c.values = static_cast<size_t>(row * (c.second ? a.side[1].token : a.side[0].token) + h * (c.second ? a.side[1].head : a.side[0].head));
   c.group = static_cast<size_t>(slot) * a.heads + h;
   return c;
@@ -62,6 +63,18 @@ __device__ __forceinline__ uint8_t* cache_codes(const CacheArgs& a, const CacheI
 }
 __device__ __forceinline__ uint8_t* cache_scales(const CacheArgs& a, const CacheItem& c) {
   return (c.second ? a.side[1].scales : a.side[0].scales) + c.group * a.scale_pitch;
+}
+// What those point into, for the checked build.
+__device__ __forceinline__ Extent cache_codes_extent(const CacheArgs& a, const CacheItem& c) {
+  return Extent::of(a.side[c.second].codes, static_cast<size_t>(a.num_slots) * a.heads * a.code_pitch);
+}
+__device__ __forceinline__ Extent cache_scales_extent(const CacheArgs& a, const CacheItem& c) {
+  return Extent::of(a.side[c.second].scales, static_cast<size_t>(a.num_slots) * a.heads * a.scale_pitch);
+}
+template <typename T>
+__device__ __forceinline__ Extent cache_values_extent(const CacheArgs& a, const CacheItem& c) {
+  const CacheSide& s = a.side[c.second];
+  return Extent::of(static_cast<const T*>(s.values), static_cast<size_t>((cache_rows(a) - 1) * s.token + (a.heads - 1) * s.head + a.D));
 }
 template <typename T>
 __device__ __forceinline__ T* cache_values(const CacheArgs& a, const CacheItem& c) {
@@ -123,11 +136,13 @@ cache_write_kernel(const CacheArgs a) {
     for (int j = 0; j < U; ++j)
 #pragma unroll
       for (int k = 0; k < V; ++k)
-        group_load<ANY>(x[j][k], cache_values<T>(a, c[j]) + k * G * E, c[j].valid ? a.D - k * G * E : 0, G, lane, a.unit, stage);
+        group_load<ANY>(x[j][k], cache_values<T>(a, c[j]) + k * G * E, c[j].valid ? a.D - k * G * E : 0, G, lane, a.unit, stage,
+                        cache_values_extent<T>(a, c[j]));
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       uint8_t* codes = cache_codes(a, c[j]);
       uint8_t* scales = cache_scales(a, c[j]);
+      const Extent of_codes = cache_codes_extent(a, c[j]), of_scales = cache_scales_extent(a, c[j]);
       if constexpr (FMT == CACHE_I8) {
         float v[V][E];
         uint32_t m = 0;
@@ -138,7 +153,7 @@ cache_write_kernel(const CacheArgs a) {
         }
         const uint32_t sb = i8_scale_byte(at.max_over_head(m));
         const float inv = inverse_scale(sb);
-        if (c[j].valid && lane == 0) *scales = static_cast<uint8_t>(sb);
+        if (c[j].valid && lane == 0 && QC_AT(of_scales, scales, 1)) *scales = static_cast<uint8_t>(sb);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           const int first = k * G * E, n = c[j].valid ? min(a.D - first, G * E) : 0;
@@ -150,9 +165,9 @@ cache_write_kernel(const CacheArgs a) {
 #pragma unroll
             for (int i = 0; i < E / 4; ++i) reinterpret_cast<uint32_t*>(group)[lane * (E / 4) + i] = w[i];
             __syncwarp();
-            store_bytes<E>(codes + first, group, n, G, lane);
+            store_bytes<E>(codes + first, group, n, G, lane, of_codes);
             __syncwarp();
-          } else if (lane * E < n) {
+          } else if (lane * E < n && QC_AT(of_codes, codes + first + lane * E, E)) {
             if constexpr (E == 8) *reinterpret_cast<uint2*>(codes + first + lane * E) = make_uint2(w[0], w[1]);
             else *reinterpret_cast<uint4*>(codes + first + lane * E) = make_uint4(w[0], w[1], w[2], w[3]);
           }
@@ -166,8 +181,8 @@ cache_write_kernel(const CacheArgs a) {
           x[j][k].unpack(v);
           const uint32_t sb = mx_scale_byte(finite_top<kBlockLanes>(v, x[j][k].top()), kCoverRoundUp);
           if (!c[j].valid || col >= a.blocks * kMxBlock) continue;
-          mx_store_codes(codes + col / 2, v, inverse_scale(sb));
-          if ((col & (kMxBlock - 1)) == 0) scales[col / kMxBlock] = static_cast<uint8_t>(sb);
+          mx_store_codes(codes + col / 2, v, inverse_scale(sb), of_codes);
+          if ((col & (kMxBlock - 1)) == 0 && QC_AT(of_scales, scales + col / kMxBlock, 1)) scales[col / kMxBlock] = static_cast<uint8_t>(sb);
         }
       }
     }
@@ -202,6 +217,7 @@ cache_read_kernel(const CacheArgs a) {
     for (int j = 0; j < U; ++j) {
       const uint8_t* codes = cache_codes(a, c[j]);
       const uint8_t* scales = cache_scales(a, c[j]);
+      const Extent of_codes = cache_codes_extent(a, c[j]), of_scales = cache_scales_extent(a, c[j]);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const int col = (k * LANES + lane) * E, n = c[j].valid ? min(E, a.D - col) : 0;
@@ -209,11 +225,12 @@ cache_read_kernel(const CacheArgs a) {
         for (int i = 0; i < E / 4; ++i) w[j][k][i] = 0u;
         sb[j][k] = kScaleOne;
         if constexpr (FMT == CACHE_I8 && ANY)
-          load_bytes<E>(raw[j][k], codes + k * LANES * E, c[j].valid ? min(a.D - k * LANES * E, LANES * E) : 0, LANES, lane);
+          load_bytes<E>(raw[j][k], codes + k * LANES * E, c[j].valid ? min(a.D - k * LANES * E, LANES * E) : 0, LANES, lane, of_codes);
         if (n <= 0) continue;
         if constexpr (FMT == CACHE_I8) {
-          sb[j][k] = __ldg(scales);
+          if (QC_AT(of_scales, scales, 1)) sb[j][k] = __ldg(scales);
           if constexpr (!ANY) {
+            if (!QC_AT(of_codes, codes + col, n)) continue;
             if (a.code_vec) {
               if constexpr (E == 8) {
                 const uint2 q = __ldg(reinterpret_cast<const uint2*>(codes + col));
@@ -229,6 +246,7 @@ cache_read_kernel(const CacheArgs a) {
             }
           }
         } else {
+          if (!QC_AT(of_scales, scales + col / kMxBlock, 1) || !QC_AT(of_codes, codes + col / 2, E / 2)) continue;
           sb[j][k] = __ldg(scales + col / kMxBlock);
           if constexpr (E == 8) {
             w[j][k][0] = __ldg(reinterpret_cast<const uint32_t*>(codes + col / 2));
@@ -258,7 +276,8 @@ cache_read_kernel(const CacheArgs a) {
         }
         Piece<T> p;
         p.pack(v);
-        group_store<ANY>(p, y + k * LANES * E, c[j].valid ? a.D - k * LANES * E : 0, LANES, lane, a.unit, stage);
+        group_store<ANY>(p, y + k * LANES * E, c[j].valid ? a.D - k * LANES * E : 0, LANES, lane, a.unit, stage,
+                         cache_values_extent<T>(a, c[j]));
       }
     }
   }

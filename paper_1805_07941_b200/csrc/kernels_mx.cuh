@@ -40,17 +40,17 @@ mx_quantize_kernel(const T* __restrict__ x, const MxGrid g, uint8_t* __restrict_
   const size_t step = static_cast<size_t>(gridDim.y) * (kMxThreads >> g.log_x);
   const bool codes_here = col < scales.blocks * kMxBlock;
   uint8_t* my_stage = stage[ANY ? threadIdx.x >> 5 : 0];
+  const Extent of_x = Extent::of(x, (g.rows - 1) * g.ld + g.K), of_codes = Extent::of(codes, g.rows * pitch);
   // every lane of a warp goes round as often as the warp's first
   const size_t warp_row = (threadIdx.x & ~31u) >> g.log_x, my_row = (threadIdx.x >> g.log_x) - warp_row;
   for (size_t base = blockIdx.y * static_cast<size_t>(kMxThreads >> g.log_x) + warp_row; base < g.rows_out; base += step) {
     const size_t r = base + my_row;
     Piece<T> p;
-    group_load<ANY>(p, x + r * g.ld + first, r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0, G, lane, g.unit, my_stage);
+    group_load<ANY>(p, x + r * g.ld + first, r < g.rows ? g.K - first : 0, G, lane, g.unit, my_stage, of_x);
     float v[E];
     p.unpack(v);
     const uint32_t s = mx_scale_byte(finite_top<kBlockLanes>(v, p.top()), round_up);
-    if (codes_here && r < g.rows && QC_IN(r * pitch + col / 2 + E / 2 - 1, g.rows * pitch))
-      mx_store_codes(codes + r * pitch + col / 2, v, inverse_scale(s));
+    if (codes_here && r < g.rows) mx_store_codes(codes + r * pitch + col / 2, v, inverse_scale(s), of_codes);
     store_scale<kBlockLanes>(scales, r, col, s, codes_here && r < g.rows_out);
   }
 }
@@ -69,6 +69,7 @@ mx_dequantize_kernel(const uint8_t* __restrict__ codes, const MxScales scales, c
   const size_t pitch = static_cast<size_t>(scales.blocks) * 16;
   const size_t step = static_cast<size_t>(gridDim.y) * (kMxThreads >> g.log_x);
   uint8_t* my_stage = stage[ANY ? threadIdx.x >> 5 : 0];
+  const Extent of_y = Extent::of(y, (g.rows - 1) * g.ld + g.K), of_codes = Extent::of(codes, g.rows * pitch);
   const size_t warp_row = (threadIdx.x & ~31u) >> g.log_x, my_row = (threadIdx.x >> g.log_x) - warp_row;
   for (size_t base = blockIdx.y * static_cast<size_t>(kMxThreads >> g.log_x) + warp_row; base < g.rows; base += step) {
     const size_t r = base + my_row;
@@ -76,7 +77,7 @@ mx_dequantize_kernel(const uint8_t* __restrict__ codes, const MxScales scales, c
     uint32_t s = kScaleOne;
     const size_t at = r * pitch + col / 2;
     const size_t sat = scales.tiles ? mx_tile_word(r, b >> 2, scales.tiles_k) + (b & 3) : r * static_cast<size_t>(scales.blocks) + b;
-    if (r < g.rows && b < scales.blocks && QC_IN(at + E / 2 - 1, g.rows * pitch) && QC_IN(sat, scales.extent)) {
+    if (r < g.rows && b < scales.blocks && QC_AT(of_codes, codes + at, E / 2) && QC_IN(sat, scales.extent)) {
       if constexpr (E == 8) w.x = __ldg(reinterpret_cast<const uint32_t*>(codes + at));
       else w = __ldg(reinterpret_cast<const uint2*>(codes + at));
       s = __ldg(scales.bytes + sat);
@@ -86,7 +87,7 @@ mx_dequantize_kernel(const uint8_t* __restrict__ codes, const MxScales scales, c
     if constexpr (E == 16) mx_decode_eight(w.y, scale_of(s), v + 8);
     Piece<T> p;
     p.pack(v);
-    group_store<ANY>(p, y + r * g.ld + first, r < g.rows && QC_IN(r * g.ld + g.K - 1, (g.rows - 1) * g.ld + g.K) ? g.K - first : 0, G, lane, g.unit, my_stage);
+    group_store<ANY>(p, y + r * g.ld + first, r < g.rows ? g.K - first : 0, G, lane, g.unit, my_stage, of_y);
   }
 }
 

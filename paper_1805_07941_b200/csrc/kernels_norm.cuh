@@ -34,6 +34,11 @@ struct NormArgs {
   MxScales scales;        // NORM_I8_ROWS: bytes alone
 };
 
+// A tensor of a call, for the checked build: rows `ld` apart of C values (x, residual, sum), or what the outputs hold.
+template <typename T> __device__ __forceinline__ Extent norm_extent(const NormArgs<T>& a, const T* p, size_t ld) {
+  return Extent::of(p, (a.rows - 1) * ld + a.C);
+}
+
 // How the threads share out rows: a row is G lanes of a warp (a power of two, at least those of a scale word), or all of the
 // block's warps (G = 32).
 struct NormPlace {
@@ -74,22 +79,23 @@ template <typename T> struct NormRaw {
 // The group's pieces from column `first` on: loaded (all of a thread's loads come before the first use) ...
 template <bool ANY, typename T>
 __device__ __forceinline__ void norm_fetch(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T>& raw) {
-  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
+  const int n = at.valid ? a.C - first : 0;
   const T* px = a.x + at.row * a.ld_x + first;
   const T* pr = a.residual + at.row * a.ld_res + first;
+  const Extent of_x = norm_extent(a, a.x, a.ld_x), of_r = norm_extent(a, a.residual, a.ld_res);
   if constexpr (ANY) {
     if (by_bytes<T>(a.unit)) {
-      load_piece(raw.x, raw.x_ends, px, n, at.G, at.lane);
-      if (a.residual) load_piece(raw.r, raw.r_ends, pr, n, at.G, at.lane);
+      load_piece(raw.x, raw.x_ends, px, n, at.G, at.lane, of_x);
+      if (a.residual) load_piece(raw.r, raw.r_ends, pr, n, at.G, at.lane, of_r);
     } else {
       with_unit(a.unit, [&](auto u) {
-        load_dealt<decltype(u)::value>(raw.x, px, n, at.G, at.lane);
-        if (a.residual) load_dealt<decltype(u)::value>(raw.r, pr, n, at.G, at.lane);
+        load_dealt<decltype(u)::value>(raw.x, px, n, at.G, at.lane, of_x);
+        if (a.residual) load_dealt<decltype(u)::value>(raw.r, pr, n, at.G, at.lane, of_r);
       });
     }
   } else {
-    group_load<false>(raw.x, px, n, at.G, at.lane, a.unit, nullptr);
-    if (a.residual) group_load<false>(raw.r, pr, n, at.G, at.lane, a.unit, nullptr);
+    group_load<false>(raw.x, px, n, at.G, at.lane, a.unit, nullptr, of_x);
+    if (a.residual) group_load<false>(raw.r, pr, n, at.G, at.lane, a.unit, nullptr, of_r);
   }
 }
 template <typename T> __device__ __forceinline__ void add_residual(Piece<T>& h, const Piece<T>& residual) {
@@ -103,8 +109,9 @@ template <typename T> __device__ __forceinline__ void add_residual(Piece<T>& h, 
 // ... and h of them: added, rounded, kept.
 template <bool ANY, typename T>
 __device__ __forceinline__ void norm_add(const NormArgs<T>& a, const NormPlace& at, int first, NormRaw<T>& raw, Piece<T>& h, uint8_t* stage) {
-  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
+  const int n = at.valid ? a.C - first : 0;
   T* ps = a.sum + at.row * a.ld_sum + first;
+  const Extent of_s = norm_extent(a, a.sum, a.ld_sum);
   if (ANY && by_bytes<T>(a.unit)) {                         // (the three may begin at different bytes of a word)
     gather_piece(raw.x, raw.x_ends, a.x + at.row * a.ld_x + first, n, at.G, at.lane, stage);
     h = raw.x;
@@ -112,18 +119,18 @@ __device__ __forceinline__ void norm_add(const NormArgs<T>& a, const NormPlace& 
       gather_piece(raw.r, raw.r_ends, a.residual + at.row * a.ld_res + first, n, at.G, at.lane, stage);
       add_residual(h, raw.r);
     }
-    if (a.sum) store_piece(h, ps, n, at.G, at.lane, stage);
+    if (a.sum) store_piece(h, ps, n, at.G, at.lane, stage, of_s);
     return;
   }
   h = raw.x;
   if (a.residual) add_residual(h, raw.r);
   if constexpr (ANY) {
     with_unit(a.unit, [&](auto u) {
-      if (a.sum) store_dealt<decltype(u)::value>(h, ps, n, at.G, at.lane);
+      if (a.sum) store_dealt<decltype(u)::value>(h, ps, n, at.G, at.lane, of_s);
       gather_dealt<decltype(u)::value>(h, at.G, at.lane, stage);
     });
   } else {
-    if (a.sum) group_store<false>(h, ps, n, at.G, at.lane, a.unit, nullptr);
+    if (a.sum) group_store<false>(h, ps, n, at.G, at.lane, a.unit, nullptr, of_s);
   }
 }
 
@@ -142,12 +149,16 @@ __device__ __forceinline__ void norm_scale(const NormArgs<T>& a, const NormPlace
   constexpr int E = Piece<T>::E;
   Piece<T> g;
   float u[E];
+  const Extent of_g = Extent::of(a.gain, a.C);
   if (a.unit_gain >= kLoadUnit) {
-    group_load<false>(g, a.gain + first, a.C - first, at.G, at.lane, a.unit_gain, nullptr);
+    group_load<false>(g, a.gain + first, a.C - first, at.G, at.lane, a.unit_gain, nullptr, of_g);
     g.unpack(u);
   } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) u[i] = first + at.lane * E + i < a.C ? to_float(a.gain[first + at.lane * E + i]) : 0.0f;
+    for (int i = 0; i < E; ++i) {
+      const int c = first + at.lane * E + i;
+      u[i] = c < a.C && QC_AT(of_g, a.gain + c, sizeof(T)) ? to_float(a.gain[c]) : 0.0f;
+    }
   }
   h.unpack(y);
 #pragma unroll
@@ -157,13 +168,14 @@ __device__ __forceinline__ void norm_scale(const NormArgs<T>& a, const NormPlace
 template <typename T>
 __device__ __forceinline__ void norm_store_i8(const NormArgs<T>& a, const NormPlace& at, int first, const float (&y)[Piece<T>::E], float inv, uint8_t* stage) {
   constexpr int E = Piece<T>::E;
-  const int n = at.valid && QC_IN(at.row, a.rows) ? a.C - first : 0;
+  const int n = at.valid ? a.C - first : 0;
   uint32_t c[E / 4];
 #pragma unroll
   for (int i = 0; i < E / 4; ++i) c[i] = i8_encode_four(y + 4 * i, inv);
   uint8_t* p = a.codes + at.row * a.C + first;
+  const Extent of_codes = Extent::of(a.codes, a.rows * a.C);
   if (a.code_vec) {                                         // (C is then a multiple of E, too)
-    if (at.lane * E >= n) return;
+    if (at.lane * E >= n || !QC_AT(of_codes, p + at.lane * E, E)) return;
     if constexpr (E == 8) *reinterpret_cast<uint2*>(p + at.lane * E) = make_uint2(c[0], c[1]);
     else *reinterpret_cast<uint4*>(p + at.lane * E) = make_uint4(c[0], c[1], c[2], c[3]);
   } else {
@@ -171,7 +183,7 @@ __device__ __forceinline__ void norm_store_i8(const NormArgs<T>& a, const NormPl
 #pragma unroll
     for (int i = 0; i < E / 4; ++i) reinterpret_cast<uint32_t*>(mine)[at.lane * (E / 4) + i] = c[i];
     __syncwarp();
-    store_bytes<E>(p, mine, min(n, at.G * E), at.G, at.lane);
+    store_bytes<E>(p, mine, min(n, at.G * E), at.G, at.lane, of_codes);
     __syncwarp();
   }
 }
@@ -182,9 +194,10 @@ __device__ __forceinline__ void norm_store_mx(const NormArgs<T>& a, const NormPl
   const int col = first + at.lane * E;
   const uint32_t s = mx_scale_byte(finite_top<kBlockLanes>(y, top_bits(y)), kCoverRoundUp);
   const int padded = a.scales.blocks * kMxBlock;
-  const bool here = at.valid && col < padded && QC_IN(at.row, a.rows);
+  const bool here = at.valid && col < padded;
   store_scale<kBlockLanes>(a.scales, at.row, col, s, here);
-  if (here) mx_store_codes(a.codes + at.row * static_cast<size_t>(padded / 2) + col / 2, y, inverse_scale(s));
+  if (here)
+    mx_store_codes(a.codes + at.row * static_cast<size_t>(padded / 2) + col / 2, y, inverse_scale(s), Extent::of(a.codes, a.rows * (padded / 2)));
 }
 
 // Scale words of the rows that fill up the last tile of 128, by `blocks` blocks of which this is number `block`.
@@ -247,7 +260,7 @@ rmsnorm_kernel(const NormArgs<T> a, int G, unsigned int row_blocks) {
       m = max(m, finite_top<1>(y[v], top_bits(y[v])));
     }
     const uint32_t s = i8_scale_byte(row_max(m, tops, at));
-    if (at.lane == 0 && at.warp == 0 && at.valid) a.scales.bytes[at.row] = static_cast<uint8_t>(s);
+    if (at.lane == 0 && at.warp == 0 && at.valid && QC_IN(at.row, a.rows)) a.scales.bytes[at.row] = static_cast<uint8_t>(s);
 #pragma unroll
     for (int v = 0; v < V; ++v) norm_store_i8(a, at, (v * at.warps + at.warp) * 32 * E, y[v], inverse_scale(s), stage);
   } else {
@@ -302,7 +315,7 @@ rmsnorm_long_kernel(const NormArgs<T> a, unsigned int row_blocks) {
     }
     const uint32_t s = i8_scale_byte(row_max(m, tops, at));
     inv = inverse_scale(s);
-    if (threadIdx.x == 0) a.scales.bytes[at.row] = static_cast<uint8_t>(s);
+    if (threadIdx.x == 0 && QC_IN(at.row, a.rows)) a.scales.bytes[at.row] = static_cast<uint8_t>(s);
   }
   for (int first = at.warp * 32 * E; first < a.C; first += kStep) {
     norm_fetch<ANY>(again, at, first, raw);

@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "epilogue.cuh"
+#include "extent.cuh"
 
 namespace qc {
 
@@ -56,6 +57,9 @@ __device__ __forceinline__ float2 unpack_two(uint32_t w, __nv_bfloat16) {
 __device__ __forceinline__ float2 unpack_two(uint32_t w, __half) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
+
+// The checked build's test of an access: whether `count` bytes from p on are the tensor's.  (Elsewhere the constant true.)
+#define QC_AT(extent, p, count) QC_IN((extent).has(p, count) ? 0 : 1, 1)
 
 constexpr uint32_t kInfBits = 0x7F800000u;
 
@@ -162,18 +166,19 @@ struct ByteRun {
 };
 // From `bytes`, shared memory (4-byte aligned, readable up to the word behind the last byte's).
 template <int E>
-__device__ __forceinline__ void store_bytes(void* to, const uint8_t* bytes, int n, int G, int lane) {
+__device__ __forceinline__ void store_bytes(void* to, const uint8_t* bytes, int n, int G, int lane, const Extent& in) {
   const ByteRun run(to, n);
   uint8_t* p = static_cast<uint8_t*>(to);
   const uint32_t* words = reinterpret_cast<const uint32_t*>(bytes);
-  if (lane < run.head) p[lane] = bytes[lane];
+  if (lane < run.head && QC_AT(in, p + lane, 1)) p[lane] = bytes[lane];
 #pragma unroll
   for (int i = 0; i < E / 4; ++i) {
     const int k = i * G + lane;
-    if (k < run.words) *reinterpret_cast<uint32_t*>(p + run.head + 4 * k) = __funnelshift_r(words[k], words[k + 1], 8 * run.head);
+    if (k < run.words && QC_AT(in, p + run.head + 4 * k, 4))
+      *reinterpret_cast<uint32_t*>(p + run.head + 4 * k) = __funnelshift_r(words[k], words[k + 1], 8 * run.head);
   }
   const int end = run.head + 4 * run.words + lane;
-  if (lane < run.tail) p[end] = bytes[end];
+  if (lane < run.tail && QC_AT(in, p + end, 1)) p[end] = bytes[end];
 }
 // As loaded: a lane's words, and its byte before the first (low) and behind the last.  Then, through the group's part of the
 // warp's shared memory, each lane's own E bytes; where there are none, anything.  Whole warps.
@@ -181,13 +186,15 @@ template <int E> struct DealtBytes {
   uint32_t w[E / 4], ends;
 };
 template <int E>
-__device__ __forceinline__ void load_bytes(DealtBytes<E>& x, const void* from, int n, int G, int lane) {
+__device__ __forceinline__ void load_bytes(DealtBytes<E>& x, const void* from, int n, int G, int lane, const Extent& in) {
   const ByteRun run(from, n);
   const uint8_t* p = static_cast<const uint8_t*>(from);
 #pragma unroll
-  for (int i = 0; i < E / 4; ++i) x.w[i] = i * G + lane < run.words ? *(reinterpret_cast<const uint32_t*>(p + run.head) + i * G + lane) : 0u;
-  x.ends = lane < run.head ? p[lane] : 0u;
-  if (lane < run.tail) x.ends |= static_cast<uint32_t>(p[run.head + 4 * run.words + lane]) << 8;
+  for (int i = 0; i < E / 4; ++i)
+    x.w[i] = i * G + lane < run.words && QC_AT(in, p + run.head + 4 * (i * G + lane), 4)
+                 ? *(reinterpret_cast<const uint32_t*>(p + run.head) + i * G + lane) : 0u;
+  x.ends = lane < run.head && QC_AT(in, p + lane, 1) ? p[lane] : 0u;
+  if (lane < run.tail && QC_AT(in, p + run.head + 4 * run.words + lane, 1)) x.ends |= static_cast<uint32_t>(p[run.head + 4 * run.words + lane]) << 8;
 }
 template <int E>
 __device__ __forceinline__ void gather_bytes(uint32_t (&w)[E / 4], const DealtBytes<E>& x, const void* from, int n, int G, int lane, uint8_t* stage) {
@@ -241,15 +248,16 @@ template <int U> __device__ __forceinline__ void set_unit(uint32_t (&w)[8], int 
 
 // Dealt pieces from p, where n values exist (zeros behind them), and back; units of U bytes.
 template <int U, typename T>
-__device__ __forceinline__ void load_dealt(Piece<T>& x, const T* p, int n, int G, int lane) {
+__device__ __forceinline__ void load_dealt(Piece<T>& x, const T* p, int n, int G, int lane, const Extent& in) {
   using Unit = typename UnitOf<U>::type;
   constexpr int kValues = U / static_cast<int>(sizeof(T));   // of a unit
 #pragma unroll
   for (int i = 0; i < 32 / U; ++i) {
     const int at = (i * G + lane) * kValues, left = n - at;
     Unit v{};
-    if (left >= kValues) v = *reinterpret_cast<const Unit*>(p + at);
-    else if (kValues > 1 && left > 0) {                      // (the row ends inside a unit)
+    if (left >= kValues) {
+      if (QC_AT(in, p + at, U)) v = *reinterpret_cast<const Unit*>(p + at);
+    } else if (kValues > 1 && left > 0 && QC_AT(in, p + at, left * sizeof(T))) {   // (the row ends inside a unit)
       T part[kValues];
 #pragma unroll
       for (int k = 0; k < kValues; ++k) part[k] = k < left ? p[at + k] : from_float<T>(0.0f);
@@ -259,15 +267,16 @@ __device__ __forceinline__ void load_dealt(Piece<T>& x, const T* p, int n, int G
   }
 }
 template <int U, typename T>
-__device__ __forceinline__ void store_dealt(const Piece<T>& x, T* p, int n, int G, int lane) {
+__device__ __forceinline__ void store_dealt(const Piece<T>& x, T* p, int n, int G, int lane, const Extent& in) {
   using Unit = typename UnitOf<U>::type;
   constexpr int kValues = U / static_cast<int>(sizeof(T));
 #pragma unroll
   for (int i = 0; i < 32 / U; ++i) {
     const int at = (i * G + lane) * kValues, left = n - at;
     const Unit v = unit_of<U>(x.w, i);
-    if (left >= kValues) *reinterpret_cast<Unit*>(p + at) = v;
-    else if (kValues > 1 && left > 0) {
+    if (left >= kValues) {
+      if (QC_AT(in, p + at, U)) *reinterpret_cast<Unit*>(p + at) = v;
+    } else if (kValues > 1 && left > 0 && QC_AT(in, p + at, left * sizeof(T))) {
       T part[kValues];
       memcpy(part, &v, U);
 #pragma unroll
@@ -313,9 +322,9 @@ template <typename T> __device__ __forceinline__ bool by_bytes(int unit) { retur
 template <typename T>
 __device__ __forceinline__ int byte_count(int n, int G) { return min(n, G * Piece<T>::E) * static_cast<int>(sizeof(T)); }
 template <typename T>
-__device__ __forceinline__ void load_piece(Piece<T>& x, uint32_t& ends, const T* p, int n, int G, int lane) {
+__device__ __forceinline__ void load_piece(Piece<T>& x, uint32_t& ends, const T* p, int n, int G, int lane, const Extent& in) {
   DealtBytes<32> dealt;
-  load_bytes<32>(dealt, p, byte_count<T>(n, G), G, lane);
+  load_bytes<32>(dealt, p, byte_count<T>(n, G), G, lane, in);
 #pragma unroll
   for (int i = 0; i < 8; ++i) x.w[i] = dealt.w[i];
   ends = dealt.ends;
@@ -333,13 +342,13 @@ __device__ __forceinline__ void gather_piece(Piece<T>& x, uint32_t ends, const T
     for (int i = 0; i < 8; ++i) x.w[i] = left >= 2 * i + 2 ? x.w[i] : left == 2 * i + 1 ? x.w[i] & 0xFFFFu : 0u;
 }
 template <typename T>
-__device__ __forceinline__ void store_piece(const Piece<T>& x, T* p, int n, int G, int lane, uint8_t* stage) {
+__device__ __forceinline__ void store_piece(const Piece<T>& x, T* p, int n, int G, int lane, uint8_t* stage, const Extent& in) {
   uint8_t* group = stage + ((threadIdx.x & 31) - lane) * 32;
   uint4* q = reinterpret_cast<uint4*>(group + lane * 32);
   q[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
   q[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
   __syncwarp();
-  store_bytes<32>(p, group, byte_count<T>(n, G), G, lane);
+  store_bytes<32>(p, group, byte_count<T>(n, G), G, lane, in);
   __syncwarp();
 }
 
@@ -347,16 +356,17 @@ __device__ __forceinline__ void store_piece(const Piece<T>& x, T* p, int n, int 
 // n exist (zeros behind them; n may be negative).  ANY: exchanged (an instantiation of its own, so that the
 // aligned one is lean).  Whole warps.
 template <bool ANY, typename T>
-__device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G, int lane, int unit, uint8_t* stage) {
+__device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G, int lane, int unit, uint8_t* stage, const Extent& in) {
   constexpr int E = Piece<T>::E;
   if constexpr (!ANY) {
     const int left = n - lane * E;
-    if (left >= E) {
+    const bool here = left > 0 && QC_AT(in, p + lane * E, min(left, E) * sizeof(T));
+    if (left >= E && here) {
       x.load(p + lane * E, unit);
     } else {
       x.clear();
       constexpr int kValues = 4 / static_cast<int>(sizeof(T));
-      if (left > 0) {                                        // the row's end, in words
+      if (here) {                                        // the row's end, in words
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if (left >= (i + 1) * kValues) x.w[i] = reinterpret_cast<const uint32_t*>(p + lane * E)[i];
@@ -367,11 +377,11 @@ __device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G
   } else {
     if (by_bytes<T>(unit)) {
       uint32_t ends;
-      load_piece(x, ends, p, n, G, lane);
+      load_piece(x, ends, p, n, G, lane, in);
       gather_piece(x, ends, p, n, G, lane, stage);
     } else {
       with_unit(unit, [&](auto u) {
-        load_dealt<decltype(u)::value>(x, p, n, G, lane);
+        load_dealt<decltype(u)::value>(x, p, n, G, lane, in);
         gather_dealt<decltype(u)::value>(x, G, lane, stage);
       });
     }
@@ -379,13 +389,14 @@ __device__ __forceinline__ void group_load(Piece<T>& x, const T* p, int n, int G
 }
 // The same way back: the first n values.
 template <bool ANY, typename T>
-__device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int G, int lane, int unit, uint8_t* stage) {
+__device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int G, int lane, int unit, uint8_t* stage, const Extent& in) {
   constexpr int E = Piece<T>::E;
   if constexpr (!ANY) {
     const int left = n - lane * E;
-    if (left >= E) {
+    const bool here = left > 0 && QC_AT(in, p + lane * E, min(left, E) * sizeof(T));
+    if (left >= E && here) {
       x.store(p + lane * E, unit);
-    } else if (left > 0) {
+    } else if (here) {
       constexpr int kValues = 4 / static_cast<int>(sizeof(T));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -395,12 +406,12 @@ __device__ __forceinline__ void group_store(const Piece<T>& x, T* p, int n, int 
     }
   } else {
     if (by_bytes<T>(unit)) {
-      store_piece(x, p, n, G, lane, stage);
+      store_piece(x, p, n, G, lane, stage, in);
     } else {
       with_unit(unit, [&](auto u) {
         Piece<T> dealt = x;
         deal<decltype(u)::value>(dealt, G, lane, stage);
-        store_dealt<decltype(u)::value>(dealt, p, n, G, lane);
+        store_dealt<decltype(u)::value>(dealt, p, n, G, lane, in);
       });
     }
   }
@@ -517,7 +528,8 @@ __device__ __forceinline__ void i8_decode_four(uint32_t w, float scale, float* v
 
 // Codes of a lane's E values in 4 bits.
 template <int E>
-__device__ __forceinline__ void mx_store_codes(uint8_t* p, const float (&v)[E], float inv) {
+__device__ __forceinline__ void mx_store_codes(uint8_t* p, const float (&v)[E], float inv, const Extent& in) {
+  if (!QC_AT(in, p, E / 2)) return;
   if constexpr (E == 8) *reinterpret_cast<uint32_t*>(p) = mx_encode_eight(v, inv);
   else *reinterpret_cast<uint2*>(p) = make_uint2(mx_encode_eight(v, inv), mx_encode_eight(v + 8, inv));
 }
@@ -532,7 +544,7 @@ struct MxScales {
 // The word of blocks 4 t .. 4 t + 3 of row r, in tiles (with the bytes behind the row's last block: a byte of 2^0 each).
 __device__ __forceinline__ void store_scale_word(const MxScales& s, size_t r, int t, uint32_t word) {
   const size_t at = mx_tile_word(r, t, s.tiles_k);
-  if (QC_IN(at + 3, s.extent)) *reinterpret_cast<uint32_t*>(s.bytes + at) = word;
+  if (QC_AT(Extent::of(s.bytes, s.extent), s.bytes + at, 4)) *reinterpret_cast<uint32_t*>(s.bytes + at) = word;
 }
 // The scale byte s of the block of which this lane's values, from column `col` of row r on, are a part.  Every lane of a warp
 // calls it (`here`: the lane has values or their padding); LANES lanes a block.
