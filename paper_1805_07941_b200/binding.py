@@ -655,6 +655,7 @@ def qquantize_bias(b, e_x, e_w):
 # ---------------------------------------------------------------------------------------------------------------
 _types = {}
 _BYTES = ()
+_INT_MAX = 0x7FFFFFFF
 _INT64 = _empty = None
 
 
@@ -709,7 +710,9 @@ def _bytes(t, count, what):
 
 
 def _mx_size(rows, K, layout):
-    """(bytes of codes in a row, bytes of all scales) of a microscaled tensor."""
+    """(bytes of codes in a row, bytes of all scales) of a microscaled tensor.  (ctypes would cut a K that does not fit an int.)"""
+    if K > _INT_MAX:
+        raise ValueError("rows of %d values are too long" % K)
     blocks = (K + 31) // 32
     return blocks * 16, (rows + 127) // 128 * ((blocks + 3) // 4) * 512 if layout == MX_TILES else rows * blocks
 
@@ -767,6 +770,8 @@ class QMXLinear:
 
     def __init__(self, w_codes, w_scales, N, K, bias=None, relu=0, dtype=None):
         import torch
+        if N > _INT_MAX:
+            raise ValueError("%d output channels are too many" % N)
         self.dtype = dtype or torch.bfloat16
         self.desc = qmx_linear_desc(N=N, K=K, relu=int(relu), type=_type_of(self.dtype))
         self._pitch, size = _mx_size(N, K, MX_TILES)
@@ -785,6 +790,8 @@ class QMXLinear:
     def run(self, x_codes, x_scales, y=None):
         """x_codes [tokens, ...], x_scales in tiles -> y [tokens, N] (contiguous rows).  Asynchronous on the current stream."""
         tokens = x_codes.shape[0]
+        if tokens > _INT_MAX:
+            raise ValueError("%d tokens are too many" % tokens)
         if y is None:
             y = _empty((tokens, self.N), dtype=self.dtype, device=x_codes.device)
         dev = _current_device()
@@ -864,8 +871,12 @@ def qrmsnorm(x, gain, eps, residual=None, sum_out=None, out=NORM_I8, e=0, layout
     if not on or codes.get_device() != dev:
         _device(x, gain, residual, sum_out, codes, scales)
     if rows and C:
-        rc = (_lib or lib()).qrmsnorm(_NORM_ARGS.pack(x.data_ptr(), residual_at, gain.data_ptr(), sum_at, type_, C, rows, ld, ld_residual, ld_sum,
-                                                      eps, out, e, layout, codes.data_ptr(), scales_at), _raw_stream(dev))
+        try:
+            args = _NORM_ARGS.pack(x.data_ptr(), residual_at, gain.data_ptr(), sum_at, type_, C, rows, ld, ld_residual, ld_sum, eps, out, e, layout,
+                                   codes.data_ptr(), scales_at)
+        except struct.error as err:
+            raise ValueError("rows of %d values, eps %r, e %r, out %r or layout %r: %s" % (C, eps, e, out, layout, err)) from None
+        rc = (_lib or lib()).qrmsnorm(args, _raw_stream(dev))
         if rc:
             _check(rc)
     return codes, scales
@@ -879,6 +890,8 @@ class QCache:
         slots, heads = k_codes.shape[:2]
         D = k_codes.shape[2] if D is None else D
         blocks = -(-D // 32)
+        if heads > _INT_MAX or D > _INT_MAX:
+            raise ValueError("%d heads of %d values are too many" % (heads, D))
         _device(k_codes, k_scales, v_codes, v_scales)
         if not _types:
             _start()
