@@ -884,11 +884,15 @@ def qrmsnorm(x, gain, eps, residual=None, sum_out=None, out=NORM_I8, e=0, layout
 
 class QCache:
     """A quantized cache of keys and values over tensors that the caller owns: codes [slots, heads, ...] and scales
-    [slots, heads, ...] of one byte each (the layout is qcache_desc's).  v_codes, v_scales None: a cache of one tensor."""
+    [slots, heads, ...] of one byte each (the layout is qcache_desc's).  v_codes, v_scales None: a cache of one tensor.  D, the
+    values of a head, may be left out for int8 codes alone: a head's 4-bit codes are whole blocks, which do not tell it."""
 
     def __init__(self, k_codes, k_scales, v_codes=None, v_scales=None, D=None, fmt=CACHE_I8):
         slots, heads = k_codes.shape[:2]
-        D = k_codes.shape[2] if D is None else D
+        if D is None:
+            if fmt != CACHE_I8:
+                raise ValueError("a cache of 4-bit codes needs D, the values of a head")
+            D = k_codes.shape[2]
         blocks = -(-D // 32)
         if heads > _INT_MAX or D > _INT_MAX:
             raise ValueError("%d heads of %d values are too many" % (heads, D))

@@ -61,3 +61,9 @@ def test_caches():
     for shape, D in (((2, WIDE, 64), 64), ((2, 1, WIDE), WIDE)):
         with pytest.raises(ValueError):
             binding.QCache(meta(*shape), meta(*shape[:2]), D=D)
+
+
+def test_a_cache_of_4_bit_codes_needs_the_values_of_a_head():
+    """The codes' width is their bytes: taken for D it would be a cache of half as many values, in another layout."""
+    with pytest.raises(ValueError, match="needs D"):
+        binding.QCache(meta(2, 1, 64), meta(2, 1, 4), fmt=binding.CACHE_MX)
