@@ -235,17 +235,16 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 
   // Both issuing warps run their loops with warp-uniform values, so that addresses, coordinates and descriptors live in
   // uniform registers, where copies and MMAs take their operands from; one lane issues.
+  int issued = 0;                                            // stages loaded (warp 0)
   if (warp == 0) {
     // ------------------------------------------------------------------ loads
     const bool leader = ptx::elect_one();
-    bool ok = true;
-    int stage = 0, issued = 0;
+    int stage = 0;
     uint32_t phase = 1;                                      // (the first pass over the ring finds every stage free)
     for (int kb = kb0; kb < kb1; ++kb, ++issued) {
       const uint32_t empty = ptx::smem_u32(&sh->empty[stage]);
       if (wait_limit == 0u || !ptx::mbar_try_wait(empty, phase)) {
-        ok = mx_wait(empty, phase, wait_limit, &sh->abort_flag, status);
-        if (!ok) break;
+        if (!mx_wait(empty, phase, wait_limit, &sh->abort_flag, status)) break;
       }
       const uint32_t bar = ptx::smem_u32(&sh->full[stage]);
       const uint32_t a = ring_addr + static_cast<uint32_t>(stage) * Tile::kStage;
@@ -257,15 +256,6 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         ptx::tma_load_2d(a + Tile::kA + Tile::kB + Tile::kSA, &map_xs, bar, kb * 256, t0 >> 7);
       }
       if (++stage == prm.stages) { stage = 0; phase ^= 1u; }
-    }
-    __syncwarp();
-    if (!ok || sh->abort_flag) {
-      // the copies already issued land before this CTA's shared memory goes away (bounded, whatever the caller's limit)
-      for (int i = 0; i < issued && i < prm.stages; ++i) {
-        const int use = issued - 1 - i, s = use % prm.stages;
-        const uint32_t parity = static_cast<uint32_t>(use / prm.stages) & 1u;
-        for (unsigned int it = 0; it < kDrainPolls && !ptx::mbar_try_wait(ptx::smem_u32(&sh->full[s]), parity); ++it) {}
-      }
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -314,6 +304,16 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   __syncthreads();                                           // (no role is still waiting: the flag is final)
   ptx::tc_fence_after();
   const bool good = sh->abort_flag == 0;
+  if (!good && warp == 0) {
+    // The copies that were issued land before this CTA's shared memory goes away (bounded, whatever the caller's limit).  Any
+    // role may have given up, also on copies of a loader that had long finished: so all of this comes after the flag is final.
+    for (int i = 0; i < issued && i < prm.stages; ++i) {
+      const int use = issued - 1 - i, s = use % prm.stages;
+      const uint32_t parity = static_cast<uint32_t>(use / prm.stages) & 1u;
+      for (unsigned int it = 0; it < kDrainPolls && !ptx::mbar_try_wait(ptx::smem_u32(&sh->full[s]), parity); ++it) {}
+    }
+    __syncwarp();
+  }
   const int n = n0 + static_cast<int>(threadIdx.x);
   const uint32_t lane_addr = tmem + (static_cast<uint32_t>(warp * 32) << 16);
   const float b = bias != nullptr && n < prm.N ? __ldg(bias + n) : 0.0f;

@@ -81,6 +81,9 @@ __device__ __forceinline__ void sts_u16(uint32_t addr, uint32_t v) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(static_cast<unsigned short>(v)) : "memory");
 }
 __device__ __forceinline__ void sts_u32(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void st_cluster_u32(uint32_t cluster_addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
@@ -235,10 +238,6 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
       }
     }
     __syncwarp();
-    // after a wait that expired the copies on their way have time to land (microseconds; their barrier is the first CTA's)
-    if (leader && (!ok || sh->abort_flag))
-      for (int i = 0; i < 256; ++i) __nanosleep(200);
-    __syncwarp();
   } else if (warp == 1) {
     if (rank == 0) {
       // ---------------------------------------------------------------- scales to tensor memory, products, for both CTAs
@@ -289,12 +288,6 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         }
         if (ok && leader) ptx::mma_commit_pair(ptx::smem_u32(&sh->acc_full[tiles & 1]));
       }
-      __syncwarp();
-      if (!ok && leader) {
-        // what was issued finishes before tensor memory and the operands go away
-        ptx::mma_commit_pair(ptx::smem_u32(&sh->drained));
-        for (unsigned int i = 0; i < kDrainPolls && !ptx::mbar_try_wait_hint(ptx::smem_u32(&sh->drained), 0u); ++i) {}
-      }
     }
     __syncwarp();
   } else {
@@ -318,7 +311,8 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
       const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16) + (buf ? kMxPairTokens : 0) + half * (kMxPairTokens / 2);
       // All of the warp's columns first, then the accumulator is given back.  The arrival is a relaxed one: what it says is
       // that the reads above are complete (tcgen05.wait::ld), and no write of this thread has to be seen by whoever waits for
-      // it; a release would wait for the stores of the tile before.
+      // it; a release would wait for the stores of the tile before.  (By the memory model alone a relaxed arrival orders
+      // nothing: this rests on the hardware, where reads that have been waited for are over and the next tile's MMAs start after the arrival.)
       uint32_t acc[kMxPairChunks][32];
 #pragma unroll
       for (int k = 0; k < kMxPairChunks; ++k) ptx::tmem_ld_32x32(lanes + 32 * k, acc[k]);
@@ -356,8 +350,21 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
   }
   // Nothing of this CTA goes away while the peer can still signal its barriers or multiply into its tensor memory.
   ptx::tc_fence_before();
-  __syncthreads();
-  ptx::cluster_sync_all();
+  __syncthreads();                                           // (no role of this CTA is still waiting: its flag is final)
+  if (threadIdx.x == 0 && sh->abort_flag) ptx::st_cluster_u32(ptx::map_to_cta(ptx::smem_u32(const_cast<int*>(&sh->abort_flag)), rank ^ 1u), 1u);
+  ptx::cluster_sync_all();                                   // (both CTAs know of a failure of either)
+  if (sh->abort_flag) {
+    // Any role of either CTA may have given up on work of others that had long issued it.  MMAs finish and copies land (in
+    // microseconds; the barriers that count them need both CTAs' parts, which may not have been issued) before the memory of either goes away.
+    if (warp == 1 && rank == 0 && ptx::elect_one()) {
+      ptx::mma_commit_pair(ptx::smem_u32(&sh->drained));
+      for (unsigned int i = 0; i < kDrainPolls && !ptx::mbar_try_wait_hint(ptx::smem_u32(&sh->drained), 0u); ++i) {}
+    }
+    if (threadIdx.x == 0)
+      for (int i = 0; i < 256; ++i) __nanosleep(200);
+    __syncthreads();
+    ptx::cluster_sync_all();
+  }
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc_pair(tmem, kMxPairCols);
