@@ -183,7 +183,8 @@ int qconv_status(qconv_handle* h);
 /* Test hook: cap on the polls of each device-side barrier wait (default 1 << 22; one poll may suspend
  * the waiting thread for up to about two microseconds, so the default gives up after seconds).  With 0 every
  * wait gives up at once: the kernel still issues the copies that need no wait, lets them land,
- * writes an undefined output (or none) and the layer's status becomes QCONV_ERR_TIMEOUT. */
+ * writes an undefined output (or none) and the layer's status becomes QCONV_ERR_TIMEOUT.  Other limits below 1 << 16 count as
+ * that many, by which everything that was issued is over. */
 int qconv_set_wait_limit(qconv_handle* h, unsigned int polls);
 
 /* Writes a one-line description of the plan (algorithm, tile shape, stages) into buf; with split=2 or 4 at its end if the last
@@ -474,7 +475,8 @@ int qmx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, long long ro
  * were captured into, which hold the address of its status word.  Device-side waits are bounded as
  * qconv_run's are; qmx_linear_status synchronises the stream of the last run (a replay's stream is the caller's to
  * synchronise first) and returns (and clears) the device status,
- * qmx_linear_set_wait_limit is the test hook that qconv_set_wait_limit is. */
+ * qmx_linear_set_wait_limit is the test hook that qconv_set_wait_limit is, with any limit (a run that gives up waits for what it
+ * issued). */
 typedef struct {
   int N, K;
   int relu;

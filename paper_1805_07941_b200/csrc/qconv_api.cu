@@ -2194,7 +2194,9 @@ int qconv_status(qconv_handle* h) {
 
 int qconv_set_wait_limit(qconv_handle* h, unsigned int polls) {
   if (!h) return fail(QCONV_ERR_BAD_ARG, "NULL handle");
-  h->wait_limit = polls;
+  // (a role that gives up does not wait for what others of its CTA have issued, other than at 0, where nothing has been: by so
+  // many polls, at least half a millisecond, all of it is over)
+  h->wait_limit = polls == 0 ? 0 : std::max(polls, 1u << 16);
   return QCONV_OK;
 }
 
