@@ -946,7 +946,8 @@ class QCache:
             _check(rc)
 
     def read(self, slots, k, v=None):
-        """The slots' keys (and values) into k (and v) [rows, heads, D]; rows whose slot is outside the cache stay as they are."""
+        """The slots' keys (and values) into k (and v) [rows, heads, D], whose rows must not overlap; rows whose slot is outside the
+        cache stay as they are."""
         rows, type_, keys, values, stream = self._args(slots, k, v)
         rc = self._read(self._desc, slots.data_ptr(), rows, keys, values, type_, stream) if rows else 0
         if rc:

@@ -10,8 +10,8 @@
 // four columns of tensor memory; the four instructions of a stage take two scales a row each out of them.  A ring
 // stage has its own place there, so that the barrier that frees the stage also says that its scales have been read.
 //
-// Bound by the bytes of the weights up to about a hundred tokens (one token x 28672 x 8192 5.8 TB/s, 0.89 of the measured copy
-// rate; x 4096 x 4096 3.6 us, of which the launch is two thirds), then by filling shared memory.
+// Bound by the bytes of the weights up to about a hundred tokens (alone, in a captured graph: one token x 28672 x 8192 5.8 TB/s, 0.89
+// of the measured copy rate; x 4096 x 4096 3.6 us, of which the launch is two thirds), then by filling shared memory.
 //
 // Roles (128 threads): warp 0 issues the loads, warp 1 owns tensor memory and issues copies and MMAs, then all four warps
 // drain a quarter of the lanes each.  With few tiles a cluster of CTAs shares a tile: each takes a part of the contraction

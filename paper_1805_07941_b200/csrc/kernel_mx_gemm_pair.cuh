@@ -1,9 +1,10 @@
 // Products of microscaled 4-bit operands (kernel_mx_gemm.cuh has the mathematics, layouts and orientation) on PAIRS of SMs:
 // a cluster of two CTAs computes tiles of 256 output channels x 192 tokens with tcgen05.mma.cta_group::2.  Each CTA loads
 // the codes of its own 128 channels and of half the tokens, the scales of its channels and of all the tokens; per
-// multiply-add that is four sevenths of the bytes of a 128 x 128 tile, and bytes are what bounds long prompts.
+// multiply-add that is 0.61 of the bytes of a 128 x 128 tile (7 / 12 of the codes'), and bytes are what bounds long prompts.
 //
-// 8192 x 8192 x 8192: 194 us, 5.7 PFLOP/s (3.4 times the measured bf16 rate).  What bounds it is filling shared memory: 31 KB a
+// 8192 x 8192 x 8192 alone, in a captured graph: 193 to 199 us, 5.6 PFLOP/s (3.4 times the measured bf16 rate); one pass among others,
+// under the power limit, 231.  What bounds it is filling shared memory: 31 KB a
 // stage at the 64 bytes a cycle an SM takes in are 496 cycles, its MMAs 384, measured 590 (without the loads 430, without the
 // scale copies 590).
 //
@@ -13,7 +14,8 @@
 // the middle of a scale tile: its scales then start two columns on.
 //
 // Outputs whose rows are 16-byte aligned and a multiple of 16 bytes long leave through shared memory and bulk stores,
-// whole rows of 128 channels; stored by the lanes a token is four pieces of 32 channels.
+// whole rows of 128 channels; stored by the lanes a token is four pieces of 32 channels (2048 x 16384 x 1024 bf16 27.2 us, with
+// 16383 channels 31.9; 8192 x 8192 x 8192 and x 8191 the same).
 //
 // Roles per CTA (320 threads): warp 0 lane 0 issues the loads, warp 1 owns tensor memory (lane 0 of the first CTA issues
 // scale copies and MMAs for both), warps 2-9 are the epilogue: tensor-memory lanes warp % 4, one half of the columns each.

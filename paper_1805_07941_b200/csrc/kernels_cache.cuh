@@ -1,9 +1,10 @@
 // Quantized caches: the values of a token's heads are converted as they are written to their slot, and read back from
 // any list of slots.  A head's D values are one group: int8 with an exponent for the group, or microscaled 4 bits.  Bound by
 // HBM on long lists and by the launch on short ones: keys and values go in one launch, a head takes LANES lanes with V
-// pieces of 32 bytes each, and a group of lanes has kCacheUnroll heads in flight and the slots of the next ones on their
-// way (slot, then codes and scales, are dependent loads).  131072 tokens x 8 heads x 128 bf16, keys and values, int8: written in
-// 146 us (0.85 of the measured copy rate), read back in 135 (0.93).
+// pieces of 32 bytes each, and a group of lanes has kCacheUnroll heads in flight and, on lists that the grid goes round more than
+// once (75776 heads of 128 16-bit values), the slots of the next ones on their way (slot, then codes and scales, are dependent
+// loads).  131072 tokens x 8 heads x 128 bf16, keys and values, int8: written in 141 us (0.88 of the measured copy rate), read back in
+// 134 (0.93); in 4 bits 126 and 120 (0.83, 0.88).
 #pragma once
 #include "cache_items.cuh"
 #include "mx_format.cuh"
@@ -82,8 +83,8 @@ __device__ __forceinline__ T* cache_values(const CacheArgs& a, const CacheItem& 
 }
 
 // How the lanes of a warp share out heads.  FEW: as few each as hold one, above LANES / 2, and the lanes behind the last
-// whole group are idle.  Else LANES each.  (32768 tokens x 8 heads of bf16 to int8, few: 80 values 29.1 us, 96 34.1, 128
-// 38.5; whole: 39.0, 39.4, 39.4.  Back, few: 30.5, 35.6, 40.9; whole: 32.5, 33.9, 36.4, so that reading has it whole.)
+// whole group are idle.  Else LANES each.  (32768 tokens x 8 heads of bf16 to int8, few: 80 values 28.8 us, 96 33.8, 128
+// 38.4; whole: 39.0, 39.4, 39.4.  Back, few: 30.5, 35.6, 40.9; whole: 32.5, 34.0, 36.3, so that reading has it whole.)
 template <int LANES, bool FEW> struct CacheLanes {
   int G, per_warp, lane;
   unsigned int mine;             // which of the warp's heads; past all items where idle
